@@ -1,6 +1,7 @@
 /*
  * sptir.h - C ABI of the hyb(c,k) composable-format SpMM library for gfx950
- * (plus SDDMM on CSR, the other sparse operator of the paper's GNN section).
+ * (plus SDDMM on CSR, the other sparse operator of the paper's GNN section, the relational operator, and the operators of a
+ * mixture-of-experts layer, where a router makes the relations).
  *
  * The operations follow the SpMM problem statement of the paper (arXiv
  * 2207.04606): A is sparse in CSR with int32 indices and float32 values, X and
@@ -496,6 +497,150 @@ sptir_status_t sptir_rgms(const sptir_rgms_t* rgms, const float* X, const float*
                           int32_t d_out, void* stream);
 sptir_status_t sptir_rgms_info(const sptir_rgms_t* rgms, sptir_rgms_info_t* out);
 sptir_status_t sptir_rgms_destroy(sptir_rgms_t* rgms); /* NULL is accepted */
+
+/*
+ * A mixture-of-experts layer: the relational operator above with the router's choice of experts as its relations, for
+ * which a handle would have to be built anew at every step.  T = n_tokens tokens choose k = top_k of E = n_experts experts
+ * each; entry t * k + j is choice j of token t, and there are N = T * k < 2^31 entries.  An entry whose expert is outside
+ * 0 .. E - 1 is dropped: it contributes nothing anywhere.  Limits of all entry points (UNSUPPORTED beyond): E <= 1024,
+ * k <= 64.  They only enqueue work on `stream`, allocate nothing, may be captured, and give the same bits for the same
+ * inputs (no atomics on values).  Matrices are row-major with a row stride (ld, in elements, at least the row's length);
+ * none of them may overlap an output unless it is said so.  All pointers are device pointers.
+ */
+typedef enum { SPTIR_F32 = 0, SPTIR_F16 = 1, SPTIR_BF16 = 2 } sptir_type_t;
+
+/* How an expert's product z becomes y.  gelu is the one with erf; swiglu takes two halves of z: silu(z[0..n)) * z[n..2n). */
+typedef enum {
+  SPTIR_ACT_NONE = 0,
+  SPTIR_ACT_RELU = 1,
+  SPTIR_ACT_GELU = 2,
+  SPTIR_ACT_SILU = 3,
+  SPTIR_ACT_SWIGLU = 4
+} sptir_activation_t;
+
+/*
+ * The entries in the order of the experts (sptir_moe_sort), ascending inside an expert: those of expert e are the rows
+ * expert_ptr[e] .. expert_ptr[e + 1) of every matrix that is "in sorted order" (N rows).  Rows from expert_ptr[E] on
+ * belong to no entry: where an operator writes a matrix in sorted order it fills them with zeros, and it never reads them.
+ */
+typedef struct {
+  int32_t n_tokens, top_k, n_experts;
+  const int32_t* expert_ptr; /* [E + 1] */
+  const int32_t* entry_of;   /* [N] the entry of a sorted row, -1 from expert_ptr[E] on */
+  const int32_t* slot_of;    /* [N] the sorted row of an entry, -1 if it is dropped */
+} sptir_moe_routing_t;
+
+/*
+ * The router.  experts[t * k + j] is the expert with the j-th largest logit of token t (ties: the lower id first), and
+ *   weights[t * k + j] = p[experts[t * k + j]], p = softmax(logits[t]), divided by the sum of the token's k weights where
+ * normalise is not 0.  An expert whose logit is -inf or NaN is not chosen; where fewer than k are left the remaining
+ * choices are -1 with weight 0 (all of them for a token whose logits are all -inf).  A NaN that the sum of the softmax
+ * runs over makes the weights of its token NaN.  logits: [T, E] of `type`, 1 <= k <= E; sums are float32.
+ */
+sptir_status_t sptir_moe_route(const void* logits, int32_t type, int64_t ld_logits, int32_t n_tokens, int32_t n_experts,
+                               int32_t top_k, int32_t normalise, int32_t* experts, float* weights, void* stream);
+/* The gradient of the logits (of their type) from that of the weights; experts and weights as sptir_moe_route gave them.
+ * d_weights of a choice -1 is not read as a value (it may be NaN). */
+sptir_status_t sptir_moe_route_backward(const void* logits, int32_t type, int64_t ld_logits, int32_t n_tokens,
+                                        int32_t n_experts, int32_t top_k, int32_t normalise, const int32_t* experts,
+                                        const float* weights, const float* d_weights, void* d_logits,
+                                        int64_t ld_d_logits, void* stream);
+
+/* Sorts the entries by expert (stable).  The arrays are those of sptir_moe_routing_t; `workspace` has
+ * sptir_moe_sort_workspace bytes (0 for small N: may then be NULL) and is free again once the call's work is done. */
+int64_t sptir_moe_sort_workspace(int64_t n_entries, int32_t n_experts);
+sptir_status_t sptir_moe_sort(const int32_t* experts, int32_t n_tokens, int32_t top_k, int32_t n_experts,
+                              int32_t* expert_ptr, int32_t* entry_of, int32_t* slot_of, void* workspace,
+                              int64_t workspace_bytes, void* stream);
+
+/* Xs[s] = X[entry_of[s] / k] (times weights[entry_of[s]] unless that is NULL): tokens into sorted order.  X: [T, width]. */
+sptir_status_t sptir_moe_gather(const sptir_moe_routing_t* routing, int32_t type, int32_t width, const void* X, int64_t ldx,
+                                const float* weights, void* Xs, int64_t ldxs, void* stream);
+/* Y[t] = residual[t] + sum_j weights[t * k + j] * Ys[slot_of[t * k + j]] over the entries that are not dropped, j ascending,
+ * in float32: back into the order of the tokens.  weights NULL: 1 (the gradient of sptir_moe_gather without weights).
+ * residual may be NULL, and may be Y itself. */
+sptir_status_t sptir_moe_combine(const sptir_moe_routing_t* routing, int32_t type, int32_t width, const void* Ys,
+                                 int64_t ldys, const float* weights, const void* residual, int64_t ld_residual, void* Y,
+                                 int64_t ldy, void* stream);
+/* The gradients of sptir_moe_combine: dYs[s] = weights[entry_of[s]] * dY[token] and d_weights[t * k + j] =
+ * <dY[t], Ys[slot_of[t * k + j]]>, 0 for a dropped entry.  weights NULL: 1.  d_weights NULL: not wanted, and Ys is not
+ * read.  (That of the residual is dY.) */
+sptir_status_t sptir_moe_combine_backward(const sptir_moe_routing_t* routing, int32_t type, int32_t width, const void* dY,
+                                          int64_t ld_dy, const void* Ys, int64_t ldys, const float* weights, void* dYs,
+                                          int64_t ld_dys, float* d_weights, void* stream);
+
+/*
+ * The experts' products.  For every sorted row s of expert e:
+ *   z = W[e] x + bias[e],  y = act(z) + residual[s],
+ * x the row s of X, or with `gather` row entry_of[s] / k of it (X in the order of the tokens).  W[e]: [wide, d_in], wide =
+ * d_out, or 2 * d_out for swiglu.  routing NULL: one expert and n_rows rows, the ordinary product of a dense layer.
+ * bias, residual and pre may be NULL; `pre` receives z, for the gradient of the activation; residual may be Y itself.
+ * Products are summed in float32 (float32 ones with the float32 matrix instructions) and rounded once.
+ * Rows that are in no expert's range are not read: what they hold (NaN) reaches nothing.
+ */
+typedef struct {
+  int32_t struct_size; /* sizeof(sptir_moe_product_t) */
+  int32_t type, activation, gather;
+  int32_t d_in, d_out;
+  int64_t n_rows; /* without routing: rows of X and Y; with it: N */
+  const void* X;
+  int64_t ldx;
+  const void* W; /* [E][wide][d_in] */
+  int64_t ldw, w_stride;
+  const void* bias; /* [E][wide] */
+  int64_t bias_stride;
+  const void* residual; /* [rows, d_out] */
+  int64_t ld_residual;
+  void* pre; /* [rows, wide] */
+  int64_t ld_pre;
+  void* Y; /* [rows, d_out] */
+  int64_t ldy;
+} sptir_moe_product_t;
+sptir_status_t sptir_moe_product(const sptir_moe_routing_t* routing, const sptir_moe_product_t* product, void* stream);
+
+/*
+ * dX[s] = W[e]^T dZ[s], in sorted order (sptir_moe_combine without weights brings it to the tokens).  With an activation
+ * the result is multiplied by its derivative at `pre`, the z of the product whose y was this product's x, so that it is
+ * that product's dZ: [rows, d_in], or [rows, 2 * d_in] for swiglu, as pre.  pre is not read without an activation.
+ */
+typedef struct {
+  int32_t struct_size;
+  int32_t type, activation, reserved;
+  int32_t d_in, d_z; /* d_z: columns of dZ and rows of W[e] */
+  int64_t n_rows;
+  const void* dZ; /* [rows, d_z] */
+  int64_t ld_dz;
+  const void* W; /* [E][d_z][d_in] */
+  int64_t ldw, w_stride;
+  const void* pre;
+  int64_t ld_pre;
+  void* dX;
+  int64_t ld_dx;
+} sptir_moe_product_dx_t;
+sptir_status_t sptir_moe_product_dx(const sptir_moe_routing_t* routing, const sptir_moe_product_dx_t* product, void* stream);
+
+/*
+ * dW[e] = sum over the rows s of expert e of dZ[s] x^T and db[e] = sum of dZ[s] (db may be NULL); zeros for an expert
+ * without rows.  `workspace`: sptir_moe_product_dw_workspace bytes (0: may be NULL), free again once the work is done.
+ */
+typedef struct {
+  int32_t struct_size;
+  int32_t type, gather, reserved;
+  int32_t d_in, d_z;
+  int64_t n_rows;
+  const void* dZ;
+  int64_t ld_dz;
+  const void* X;
+  int64_t ldx;
+  void* dW; /* [E][d_z][d_in] */
+  int64_t ld_dw, dw_stride;
+  void* db; /* [E][d_z] */
+  int64_t db_stride;
+  void* workspace;
+  int64_t workspace_bytes;
+} sptir_moe_product_dw_t;
+int64_t sptir_moe_product_dw_workspace(int64_t n_rows, int32_t n_experts, int32_t d_in, int32_t d_z);
+sptir_status_t sptir_moe_product_dw(const sptir_moe_routing_t* routing, const sptir_moe_product_dw_t* product, void* stream);
 
 /* Releases the handle and its device arrays.  NULL is accepted.  Under the default allocator it waits for the device, as
  * hipFree does, and like hipFree it may be called while a stream is captured in relaxed mode only. */

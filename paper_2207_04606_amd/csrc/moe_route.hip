@@ -1,0 +1,356 @@
+// The router of a mixture-of-experts layer: softmax over the experts' logits, the top_k largest of them, and the gradient;
+// and the entries sorted by expert.
+#include <algorithm>
+
+#include "moe.h"
+
+namespace sptir {
+
+sptir_status_t moe_check_sizes(int32_t n_tokens, int32_t top_k, int32_t n_experts) {
+  if (n_tokens < 0 || top_k < 1 || n_experts < 1) return SPTIR_ERR_INVALID_ARG;
+  if (top_k > kMoeMaxTopK || n_experts > kMoeMaxExperts) return SPTIR_ERR_UNSUPPORTED;
+  if ((int64_t)n_tokens * top_k >= (int64_t)INT32_MAX) return SPTIR_ERR_OVERFLOW;
+  return SPTIR_OK;
+}
+
+sptir_status_t moe_check_routing(const sptir_moe_routing_t* r) {
+  const sptir_status_t st = moe_check_sizes(r->n_tokens, r->top_k, r->n_experts);
+  if (st != SPTIR_OK) return st;
+  if (!r->expert_ptr || (r->n_tokens > 0 && (!r->entry_of || !r->slot_of))) return SPTIR_ERR_INVALID_ARG;
+  return SPTIR_OK;
+}
+
+namespace {
+
+__device__ inline float wave_max(float v) {
+  for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+__device__ inline float wave_sum(float v) {
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+// A wavefront per token; lane l has the experts l * C .. l * C + C - 1, so that the lowest lane with the largest logit has
+// the lowest id.
+template <typename T, int C>
+__global__ __launch_bounds__(256) void k_moe_route(const T* __restrict__ logits, int64_t ld, int32_t n_tokens, int32_t n_experts,
+                                                   int32_t top_k, int32_t normalise, int32_t* __restrict__ experts,
+                                                   float* __restrict__ weights) {
+  const int lane = threadIdx.x & 63;
+  const int t = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t >= n_tokens) return;
+  const T* row = logits + (int64_t)t * ld;
+  float l[C];
+  float top = -INFINITY;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int e = lane * C + c;
+    l[c] = e < n_experts ? to_float(row[e]) : -INFINITY;
+    top = fmaxf(top, l[c]);  // (not the NaN)
+  }
+  top = wave_max(top);
+  float all = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    if (lane * C + c < n_experts) all += l[c] == -INFINITY ? 0.f : expf(l[c] - top);
+    if (!(l[c] > -INFINITY)) l[c] = -INFINITY;
+  }
+  all = wave_sum(all);
+  float mine = -INFINITY;  // the choice of this lane's number
+  int id = -1;
+  for (int j = 0; j < top_k; ++j) {
+    float best = -INFINITY;
+    int at = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (l[c] > best) { best = l[c]; at = c; }
+    const float most = wave_max(best);
+    if (most == -INFINITY) break;
+    const int owner = __ffsll((unsigned long long)__ballot(best == most)) - 1;
+    const int e = __shfl(lane * C + at, owner);
+    if (lane == j) { mine = most; id = e; }
+    if (lane == owner) {
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        if (c == at) l[c] = -INFINITY;
+    }
+  }
+  float w = id >= 0 ? expf(mine - top) : 0.f;
+  const float total = normalise ? wave_sum(w) : all;
+  if (id >= 0) w /= total;
+  if (lane < top_k) {
+    experts[(int64_t)t * top_k + lane] = id;
+    weights[(int64_t)t * top_k + lane] = w;
+  }
+}
+
+// dl[e] = [e chosen] w (dw - mean), mean = sum w dw over the choices; without normalise dl[e] = [e chosen] w dw - p[e] mean
+template <typename T, int C>
+__global__ __launch_bounds__(256) void k_moe_route_backward(const T* __restrict__ logits, int64_t ld, int32_t n_tokens,
+                                                            int32_t n_experts, int32_t top_k, int32_t normalise,
+                                                            const int32_t* __restrict__ experts,
+                                                            const float* __restrict__ weights,
+                                                            const float* __restrict__ d_weights, T* __restrict__ d_logits,
+                                                            int64_t ld_d) {
+  const int lane = threadIdx.x & 63;
+  const int t = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t >= n_tokens) return;
+  int id = -1;
+  float w = 0.f, dw = 0.f;
+  if (lane < top_k) {
+    id = experts[(int64_t)t * top_k + lane];
+    if (id >= 0) {
+      w = weights[(int64_t)t * top_k + lane];
+      dw = d_weights[(int64_t)t * top_k + lane];
+    }
+  }
+  const float mean = wave_sum(w * dw);
+  float d[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) d[c] = 0.f;
+  if (!normalise) {
+    const T* row = logits + (int64_t)t * ld;
+    float l[C], top = -INFINITY, all = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int e = lane * C + c;
+      l[c] = e < n_experts ? to_float(row[e]) : -INFINITY;
+      top = fmaxf(top, l[c]);
+    }
+    top = wave_max(top);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      l[c] = l[c] == -INFINITY ? 0.f : expf(l[c] - top);
+      all += l[c];
+    }
+    all = wave_sum(all);
+    if (all != 0.f) {  // (a token without any choice: 0)
+#pragma unroll
+      for (int c = 0; c < C; ++c) d[c] = -(l[c] / all) * mean;
+    }
+  }
+  const float of_choice = normalise ? w * (dw - mean) : w * dw;
+  for (int j = 0; j < top_k; ++j) {
+    const int e = __shfl(id, j);
+    const float g = __shfl(of_choice, j);
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (e == lane * C + c) d[c] += g;
+  }
+  T* out = d_logits + (int64_t)t * ld_d;
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+    if (lane * C + c < n_experts) out[lane * C + c] = from_float<T>(d[c]);
+}
+
+template <typename F>
+void with_columns(int32_t n_experts, F&& f) {
+  if (n_experts <= 64) f(std::integral_constant<int, 1>{});
+  else if (n_experts <= 128) f(std::integral_constant<int, 2>{});
+  else if (n_experts <= 256) f(std::integral_constant<int, 4>{});
+  else if (n_experts <= 512) f(std::integral_constant<int, 8>{});
+  else f(std::integral_constant<int, 16>{});
+}
+
+// ------------------------------------------------------------------- sort by expert
+// A stable counting sort.  The entries are cut into one contiguous part per workgroup, and that into one per wavefront; a
+// wavefront counts its entries per expert in LDS, the counts become first places (experts ascending, inside an expert
+// parts ascending), and the wavefront then places its entries in order, 64 at a time: those of one expert are found with a
+// ballot per bit of the expert's number.  With more than one workgroup the counts of all of them come from a launch before.
+__device__ inline unsigned long long lanes_alike(int e, int bits) {
+  unsigned long long m = ~0ull;
+  for (int b = 0; b < bits; ++b) {
+    const unsigned long long s = __ballot((e >> b) & 1);
+    m &= (e >> b) & 1 ? s : ~s;
+  }
+  return m;
+}
+
+__global__ __launch_bounds__(1024) void k_moe_count(const int32_t* __restrict__ experts, int64_t n, int64_t part, int32_t n_experts,
+                                                    int32_t* __restrict__ counts) {
+  extern __shared__ int32_t count[];
+  for (int e = threadIdx.x; e < n_experts; e += blockDim.x) count[e] = 0;
+  __syncthreads();
+  const int64_t lo = blockIdx.x * part, hi = min(n, lo + part);
+  for (int64_t i = lo + threadIdx.x; i < hi; i += blockDim.x) {
+    const int e = experts[i];
+    if (e >= 0 && e < n_experts) atomicAdd(&count[e], 1);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < n_experts; e += blockDim.x) counts[(int64_t)blockIdx.x * n_experts + e] = count[e];
+}
+
+__global__ __launch_bounds__(1024) void k_moe_place(const int32_t* __restrict__ experts, int64_t n, int64_t part, int32_t n_experts,
+                                                    const int32_t* __restrict__ counts, int32_t* __restrict__ expert_ptr,
+                                                    int32_t* __restrict__ entry_of, int32_t* __restrict__ slot_of) {
+  extern __shared__ int32_t place[];  // [waves][n_experts], then the expert's total, [n_experts]
+  __shared__ int32_t wave_total[16];
+  const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  int32_t* mine = place + wave * n_experts;
+  int32_t* total = place + waves * n_experts;
+  for (int i = threadIdx.x; i < waves * n_experts; i += blockDim.x) place[i] = 0;
+  __syncthreads();
+  const int64_t lo = blockIdx.x * part, hi = min(n, lo + part);
+  const int64_t seg = ((hi - lo + waves - 1) / waves + 63) / 64 * 64;
+  const int64_t w_lo = lo + wave * seg, w_hi = min(hi, w_lo + seg);
+  for (int64_t i = w_lo + lane; i < w_hi; i += 64) {
+    const int e = experts[i];
+    if (e >= 0 && e < n_experts) atomicAdd(&mine[e], 1);
+  }
+  __syncthreads();
+  // an expert's first places inside the workgroup, and its total over all workgroups
+  for (int e = threadIdx.x; e < n_experts; e += blockDim.x) {
+    int before = 0, all = 0;
+    if (counts) {
+      for (int g = 0; g < (int)gridDim.x; ++g) {
+        const int c = counts[(int64_t)g * n_experts + e];
+        if (g < (int)blockIdx.x) before += c;
+        all += c;
+      }
+    }
+    int at = before;
+    for (int w = 0; w < waves; ++w) {
+      const int c = place[w * n_experts + e];
+      place[w * n_experts + e] = at;
+      at += c;
+    }
+    total[e] = counts ? all : at;
+  }
+  __syncthreads();
+  // exclusive scan of the totals; kMoeMaxExperts = 1024 may be more than the workgroup has threads
+  int running = 0;
+  for (int e0 = 0; e0 < n_experts; e0 += blockDim.x) {
+    const int e = e0 + threadIdx.x;
+    const int c = e < n_experts ? total[e] : 0;
+    int s = c;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(s, d);
+      if (lane >= d) s += o;
+    }
+    if (lane == 63) wave_total[wave] = s;
+    __syncthreads();
+    int base = running;
+    for (int w = 0; w < waves; ++w) {
+      if (w < wave) base += wave_total[w];
+      running += wave_total[w];
+    }
+    if (e < n_experts) total[e] = base + s - c;
+    __syncthreads();
+  }
+  for (int e = threadIdx.x; e < n_experts; e += blockDim.x) {
+    const int first = total[e];
+    if (blockIdx.x == 0) expert_ptr[e] = first;
+    for (int w = 0; w < waves; ++w) place[w * n_experts + e] += first;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) expert_ptr[n_experts] = running;
+  __syncthreads();
+  const int bits = 32 - __clz(n_experts);  // (n_experts itself stands for "dropped")
+  for (int64_t i0 = w_lo; i0 < w_hi; i0 += 64) {
+    const int64_t i = i0 + lane;
+    int e = n_experts;
+    if (i < w_hi) {
+      const int given = experts[i];
+      if (given >= 0 && given < n_experts) e = given;
+    }
+    const unsigned long long same = lanes_alike(e, bits);
+    const int rank = __popcll(same & ((1ull << lane) - 1));
+    int slot = -1;
+    if (e < n_experts) slot = mine[e] + rank;
+    __builtin_amdgcn_wave_barrier();
+    if (e < n_experts && rank == 0) mine[e] += __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+    if (i < w_hi) {
+      slot_of[i] = slot;
+      if (slot >= 0) entry_of[slot] = (int32_t)i;
+    }
+  }
+  for (int64_t s = running + (int64_t)blockIdx.x * blockDim.x + threadIdx.x; s < n; s += (int64_t)gridDim.x * blockDim.x)
+    entry_of[s] = -1;
+}
+
+// entries of a workgroup: one workgroup up to 16 K (a launch less), then at most 128 workgroups (each adds up the counts of all)
+constexpr int64_t kSortAlone = 16384, kSortPart = 4096;
+constexpr int kSortGroups = 128;
+int64_t sort_part(int64_t n) {
+  if (n <= kSortAlone) return std::max<int64_t>(n, 1);
+  return std::max<int64_t>(kSortPart, ((n + kSortGroups - 1) / kSortGroups + 63) / 64 * 64);
+}
+
+}  // namespace
+}  // namespace sptir
+
+using namespace sptir;
+
+extern "C" sptir_status_t sptir_moe_route(const void* logits, int32_t type, int64_t ld_logits, int32_t n_tokens, int32_t n_experts,
+                                          int32_t top_k, int32_t normalise, int32_t* experts, float* weights, void* stream) {
+  if (!moe_type_ok(type)) return SPTIR_ERR_INVALID_ARG;
+  const sptir_status_t st = moe_check_sizes(n_tokens, top_k, n_experts);
+  if (st != SPTIR_OK) return st;
+  if (top_k > n_experts || ld_logits < n_experts) return SPTIR_ERR_INVALID_ARG;
+  if (n_tokens == 0) return SPTIR_OK;
+  if (!logits || !experts || !weights) return SPTIR_ERR_INVALID_ARG;
+  const dim3 grid((n_tokens + 3) / 4);
+  moe_with_type(type, [&](auto v) {
+    using T = decltype(v);
+    with_columns(n_experts, [&](auto c) {
+      hipLaunchKernelGGL((k_moe_route<T, decltype(c)::value>), grid, dim3(256), 0, (hipStream_t)stream, (const T*)logits, ld_logits,
+                         n_tokens, n_experts, top_k, normalise, experts, weights);
+    });
+  });
+  SPTIR_HIP(hipGetLastError());
+  return SPTIR_OK;
+}
+
+extern "C" sptir_status_t sptir_moe_route_backward(const void* logits, int32_t type, int64_t ld_logits, int32_t n_tokens,
+                                                   int32_t n_experts, int32_t top_k, int32_t normalise, const int32_t* experts,
+                                                   const float* weights, const float* d_weights, void* d_logits,
+                                                   int64_t ld_d_logits, void* stream) {
+  if (!moe_type_ok(type)) return SPTIR_ERR_INVALID_ARG;
+  const sptir_status_t st = moe_check_sizes(n_tokens, top_k, n_experts);
+  if (st != SPTIR_OK) return st;
+  if (top_k > n_experts || ld_logits < n_experts || ld_d_logits < n_experts) return SPTIR_ERR_INVALID_ARG;
+  if (n_tokens == 0) return SPTIR_OK;
+  if (!logits || !experts || !weights || !d_weights || !d_logits || d_logits == logits) return SPTIR_ERR_INVALID_ARG;
+  const dim3 grid((n_tokens + 3) / 4);
+  moe_with_type(type, [&](auto v) {
+    using T = decltype(v);
+    with_columns(n_experts, [&](auto c) {
+      hipLaunchKernelGGL((k_moe_route_backward<T, decltype(c)::value>), grid, dim3(256), 0, (hipStream_t)stream, (const T*)logits,
+                         ld_logits, n_tokens, n_experts, top_k, normalise, experts, weights, d_weights, (T*)d_logits, ld_d_logits);
+    });
+  });
+  SPTIR_HIP(hipGetLastError());
+  return SPTIR_OK;
+}
+
+extern "C" int64_t sptir_moe_sort_workspace(int64_t n_entries, int32_t n_experts) {
+  if (n_entries <= kSortAlone || n_experts < 1) return 0;
+  const int64_t part = sort_part(n_entries);
+  return (n_entries + part - 1) / part * n_experts * (int64_t)sizeof(int32_t);
+}
+
+extern "C" sptir_status_t sptir_moe_sort(const int32_t* experts, int32_t n_tokens, int32_t top_k, int32_t n_experts,
+                                         int32_t* expert_ptr, int32_t* entry_of, int32_t* slot_of, void* workspace,
+                                         int64_t workspace_bytes, void* stream) {
+  const sptir_status_t st = moe_check_sizes(n_tokens, top_k, n_experts);
+  if (st != SPTIR_OK) return st;
+  const int64_t n = (int64_t)n_tokens * top_k;
+  if (!expert_ptr || (n > 0 && (!experts || !entry_of || !slot_of))) return SPTIR_ERR_INVALID_ARG;
+  const int64_t need = sptir_moe_sort_workspace(n, n_experts);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return SPTIR_ERR_INVALID_ARG;
+  const int64_t part = sort_part(n);
+  const int groups = (int)std::max<int64_t>(1, (n + part - 1) / part);
+  // 16 wavefronts, fewer where there is less for them than 64 entries each
+  const int waves = (int)std::min<int64_t>(16, std::max<int64_t>(4, (part + 63) / 64));
+  if (groups > 1)
+    hipLaunchKernelGGL(k_moe_count, dim3(groups), dim3(1024), n_experts * sizeof(int32_t), (hipStream_t)stream, experts, n, part,
+                       n_experts, (int32_t*)workspace);
+  static OncePerDevice allowed;
+  const size_t lds = (size_t)(waves + 1) * n_experts * sizeof(int32_t);
+  allow_dynamic_lds((const void*)k_moe_place, lds, allowed);
+  hipLaunchKernelGGL(k_moe_place, dim3(groups), dim3(64 * waves), lds, (hipStream_t)stream, experts, n, part, n_experts,
+                     groups > 1 ? (const int32_t*)workspace : nullptr, expert_ptr, entry_of, slot_of);
+  SPTIR_HIP(hipGetLastError());
+  return SPTIR_OK;
+}
