@@ -17,8 +17,9 @@ enum MoeOp { kMoeForward, kMoeDx, kMoeDw };
 
 struct MoeProduct {
   const int32_t* expert_ptr;  // NULL: one expert with all rows
-  const int32_t* entry_of;    // row of x: entry_of[s] / top_k; NULL: s
-  int32_t top_k, n_experts;
+  const int32_t* entry_of;    // row of x: the entry's token; NULL: s
+  uint32_t k_mul, k_shift;    // x / top_k = (x * k_mul >> 32) >> k_shift for 0 <= x < 2^31 (k_mul 0: x)
+  int32_t n_experts;
   int64_t n_rows;
   int32_t n_i, n_j, n_r;      // sizes of an expert's product; the one over sorted rows is not used
   const void* A;              // x or dZ
@@ -83,7 +84,19 @@ inline int64_t moe_most_tiles(int64_t n_rows, int32_t n_experts, bool routed, in
   return std::min<int64_t>(n_rows, n_rows / rows + n_experts + 1);
 }
 
-__device__ inline int64_t moe_x_row(const MoeProduct& p, int64_t s) { return p.entry_of ? p.entry_of[s] / p.top_k : s; }
+__device__ inline int64_t moe_x_row(const MoeProduct& p, int64_t s) {
+  if (!p.entry_of) return s;
+  const uint32_t x = (uint32_t)p.entry_of[s];
+  return p.k_mul ? __umulhi(x, p.k_mul) >> p.k_shift : x;
+}
+// With 2^(b - 1) < k <= 2^b and m = floor(2^(31 + b) / k) + 1, m k = 2^(31 + b) + d, 0 < d <= k <= 2^b: x m / 2^(31 + b) exceeds
+// x / k by x d / (k 2^(31 + b)) < 1 / k, which moves no quotient of an x < 2^31.  m < 2^32 from k = 2 on; 0 stands for k = 1.
+inline void moe_divide_by(int32_t k, uint32_t* mul, uint32_t* shift) {
+  int b = 1;
+  while ((1 << b) < k) ++b;
+  *mul = k == 1 ? 0 : (uint32_t)((((uint64_t)1 << (31 + b)) / (uint64_t)k) + 1);
+  *shift = (uint32_t)(b - 1);
+}
 
 // ------------------------------------------------------------------- matrix instructions
 typedef float f32x4 __attribute__((ext_vector_type(4)));

@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include "moe_product.h"
+#include "moe_tiles.h"
 
 namespace sptir {
 namespace {
@@ -196,14 +197,13 @@ sptir_status_t take_routing(const sptir_moe_routing_t* routing, int64_t n_rows, 
   if (n_rows < 0 || n_rows >= (int64_t)INT32_MAX) return n_rows < 0 ? SPTIR_ERR_INVALID_ARG : SPTIR_ERR_OVERFLOW;
   p->n_rows = n_rows;
   p->n_experts = 1;
-  p->top_k = 1;
   if (!routing) return gather ? SPTIR_ERR_INVALID_ARG : SPTIR_OK;
   const sptir_status_t st = moe_check_routing(routing);
   if (st != SPTIR_OK) return st;
   if (n_rows != (int64_t)routing->n_tokens * routing->top_k) return SPTIR_ERR_INVALID_ARG;
   p->expert_ptr = routing->expert_ptr;
   p->entry_of = gather ? routing->entry_of : nullptr;
-  p->top_k = routing->top_k;
+  moe_divide_by(routing->top_k, &p->k_mul, &p->k_shift);
   p->n_experts = routing->n_experts;
   return SPTIR_OK;
 }
@@ -242,6 +242,10 @@ extern "C" sptir_status_t sptir_moe_product(const sptir_moe_routing_t* routing, 
   p.residual = q->residual; p.ld_residual = q->ld_residual;
   p.pre = q->pre; p.ld_pre = q->ld_pre;
   p.C = q->Y; p.ldc = q->ldy;
+  if (q->type != SPTIR_F32 && q->d_in > 0 &&
+      moe_words(q->type, q->d_in, {p.A, p.B}, {p.lda, p.ldb, p.b_stride}) &&
+      moe_words(q->type, q->d_out, {p.bias, p.residual, p.pre, p.C}, {p.bias_stride, p.residual ? p.ld_residual : 0, p.pre ? p.ld_pre : 0, p.ldc}))
+    return moe_tiles_forward(q->type, q->activation, p, (hipStream_t)stream);
   return launch_product<kMoeForward>(q->type, q->activation, p, (hipStream_t)stream);
 }
 
@@ -264,6 +268,9 @@ extern "C" sptir_status_t sptir_moe_product_dx(const sptir_moe_routing_t* routin
   p.B = q->W; p.ldb = q->ldw; p.b_stride = p.n_experts > 1 ? q->w_stride : 0;
   p.pre = const_cast<void*>(q->pre); p.ld_pre = q->ld_pre;
   p.C = q->dX; p.ldc = q->ld_dx;
+  if (q->type != SPTIR_F32 && q->d_z > 0 &&
+      moe_words(q->type, q->d_z, {p.A, p.B}, {p.lda, p.ldb, p.b_stride}) && moe_words(q->type, q->d_in, {act ? p.pre : nullptr, p.C}, {act ? p.ld_pre : 0, p.ldc}))
+    return moe_tiles_dx(q->type, q->activation, p, (hipStream_t)stream);
   return launch_product<kMoeDx>(q->type, q->activation, p, (hipStream_t)stream);
 }
 
@@ -296,5 +303,8 @@ extern "C" sptir_status_t sptir_moe_product_dw(const sptir_moe_routing_t* routin
     });
     SPTIR_HIP(hipGetLastError());
   }
+  if (q->type != SPTIR_F32 && q->d_in > 0 && moe_words(q->type, q->d_z, {p.A}, {p.lda}) &&
+      moe_words(q->type, q->d_in, {p.B, p.C}, {p.ldb, p.ldc, p.c_stride}))
+    return moe_tiles_dw(q->type, p, (hipStream_t)stream);
   return launch_product<kMoeDw>(q->type, SPTIR_ACT_NONE, p, (hipStream_t)stream);
 }
