@@ -134,19 +134,19 @@ __device__ inline void moe_emit(const MoeProduct& p, int expert, int64_t i, int3
   if constexpr (kOp == kMoeForward) {
     if (p.bias) acc += to_float(((const T*)p.bias)[expert * p.bias_stride + j]);
     if (p.pre) ((T*)p.pre)[i * p.ld_pre + j] = from_float<T>(acc);
-    float y = act_value<kAct>(acc);
+    float y = act_value<kAct, T>(acc);
     if (p.residual) y += to_float(((const T*)p.residual)[i * p.ld_residual + j]);
     ((T*)p.C)[i * p.ldc + j] = from_float<T>(y);
   } else if constexpr (kOp == kMoeDx) {
     if constexpr (kAct == SPTIR_ACT_SWIGLU) {
       const T* z = (const T*)p.pre + i * p.ld_pre + j;
       float dg, du;
-      act_gated_slope(acc, to_float(z[0]), to_float(z[p.n_j]), &dg, &du);
+      act_gated_slope<T>(acc, to_float(z[0]), to_float(z[p.n_j]), &dg, &du);
       T* out = (T*)p.C + i * p.ldc + j;
       out[0] = from_float<T>(dg);
       out[p.n_j] = from_float<T>(du);
     } else {
-      if constexpr (kAct != SPTIR_ACT_NONE) acc = act_slope<kAct>(acc, to_float(((const T*)p.pre)[i * p.ld_pre + j]));
+      if constexpr (kAct != SPTIR_ACT_NONE) acc = act_slope<kAct, T>(acc, to_float(((const T*)p.pre)[i * p.ld_pre + j]));
       ((T*)p.C)[i * p.ldc + j] = from_float<T>(acc);
     }
   } else {
@@ -167,7 +167,7 @@ __device__ inline void moe_emit_gated(const MoeProduct& p, int expert, int64_t i
     z[0] = from_float<T>(g);
     z[n] = from_float<T>(u);
   }
-  float y = act_gated(g, u);
+  float y = act_gated<T>(g, u);
   if (p.residual) y += to_float(((const T*)p.residual)[i * p.ld_residual + j]);
   ((T*)p.C)[i * p.ldc + j] = from_float<T>(y);
 }

@@ -208,6 +208,12 @@ sptir_status_t take_routing(const sptir_moe_routing_t* routing, int64_t n_rows, 
   return SPTIR_OK;
 }
 
+// Microseconds of k_moe_product, forward
+double small_tiles_estimate(int32_t type, const MoeProduct& p) {
+  const double rows = (double)p.n_rows + (p.expert_ptr ? std::min<double>(p.n_rows, 0.5 * kBM * p.n_experts) : 0.0);
+  return 10.0 + 2.0 * rows * p.n_j * p.n_r / (type == SPTIR_F32 ? 50e6 : 200e6);
+}
+
 bool act_ok(int32_t act) { return act >= SPTIR_ACT_NONE && act <= SPTIR_ACT_SWIGLU; }
 // Weights that are read may be shared by experts (stride 0); where they are written, neither rows nor matrices overlap.
 bool weights_ok(int64_t ld, int64_t stride, int64_t cols) { return ld >= cols && stride >= 0; }
@@ -242,10 +248,16 @@ extern "C" sptir_status_t sptir_moe_product(const sptir_moe_routing_t* routing, 
   p.residual = q->residual; p.ld_residual = q->ld_residual;
   p.pre = q->pre; p.ld_pre = q->ld_pre;
   p.C = q->Y; p.ldc = q->ldy;
-  if (q->type != SPTIR_F32 && q->d_in > 0 &&
-      moe_words(q->type, q->d_in, {p.A, p.B}, {p.lda, p.ldb, p.b_stride}) &&
-      moe_words(q->type, q->d_out, {p.bias, p.residual, p.pre, p.C}, {p.bias_stride, p.residual ? p.ld_residual : 0, p.pre ? p.ld_pre : 0, p.ldc}))
-    return moe_tiles_forward(q->type, q->activation, p, (hipStream_t)stream);
+  const int64_t x_rows = q->gather ? routing->n_tokens : p.n_rows;
+  const bool tiles = q->type != SPTIR_F32 && q->d_in > 0 && moe_near(x_rows, p.lda) && moe_near(wide, p.ldb) &&
+                     moe_words(q->type, q->d_in, {p.A, p.B}, {p.lda, p.ldb, p.b_stride}) &&
+                     moe_words(q->type, q->d_out, {p.bias, p.residual, p.pre, p.C},
+                               {p.bias_stride, p.residual ? p.ld_residual : 0, p.pre ? p.ld_pre : 0, p.ldc});
+  int32_t fragments = 1;
+  const double few_us = moe_few_estimate(q->type, p, &fragments);
+  if (few_us < (tiles ? moe_tiles_forward_estimate(q->activation, p) : small_tiles_estimate(q->type, p)))
+    return moe_few_forward(q->type, q->activation, p, fragments, (hipStream_t)stream);
+  if (tiles) return moe_tiles_forward(q->type, q->activation, p, (hipStream_t)stream);
   return launch_product<kMoeForward>(q->type, q->activation, p, (hipStream_t)stream);
 }
 
@@ -268,7 +280,7 @@ extern "C" sptir_status_t sptir_moe_product_dx(const sptir_moe_routing_t* routin
   p.B = q->W; p.ldb = q->ldw; p.b_stride = p.n_experts > 1 ? q->w_stride : 0;
   p.pre = const_cast<void*>(q->pre); p.ld_pre = q->ld_pre;
   p.C = q->dX; p.ldc = q->ld_dx;
-  if (q->type != SPTIR_F32 && q->d_z > 0 &&
+  if (q->type != SPTIR_F32 && q->d_z > 0 && moe_near(p.n_rows, p.lda) &&
       moe_words(q->type, q->d_z, {p.A, p.B}, {p.lda, p.ldb, p.b_stride}) && moe_words(q->type, q->d_in, {act ? p.pre : nullptr, p.C}, {act ? p.ld_pre : 0, p.ldc}))
     return moe_tiles_dx(q->type, q->activation, p, (hipStream_t)stream);
   return launch_product<kMoeDx>(q->type, q->activation, p, (hipStream_t)stream);

@@ -6,42 +6,73 @@
 
 namespace sptir {
 
-// Workgroup `id` of `total` takes tile moe_deal: the workgroups of an XCD (id % 8) have neighbouring tiles, so that its L2
-// serves the operands they share.
-__device__ inline int64_t moe_deal(int64_t id, int64_t total) {
-  const int64_t each = total / 8, more = total % 8, xcd = id % 8;
-  return xcd * each + min(xcd, more) + id / 8;
+// Tile of a workgroup's turn, id = turn * 256 + workgroup: 256 neighbouring tiles are worked on at once, 32 of them, next to
+// each other, by the workgroups of an XCD (workgroup % 8), whose L2 serves the operands they share.  (Experts differ in
+// rows: dealing out whole experts would leave XCDs waiting for others.)
+__device__ inline uint32_t moe_deal(uint32_t id, uint32_t total) {
+  const uint32_t turn = id & ~255u, here = id & 255u, many = min(256u, total - turn);
+  const uint32_t each = many / 8, more = many % 8, xcd = here % 8;
+  return turn + xcd * each + min(xcd, more) + here / 8;
 }
-// Tiles in bands of eight rows, down the band's columns: 32 workgroups at a time share 8 rows and 4 columns.
-__device__ inline void moe_square(int64_t id, int rows, int cols, int* row, int* col) {
-  constexpr int kBand = 8;
-  const int band = (int)(id / ((int64_t)kBand * cols)), in = (int)(id % ((int64_t)kBand * cols));
-  const int high = min(kBand, rows - band * kBand);
+// Tiles in bands of eight rows, down the band's columns: 32 at a time share 8 rows and 4 columns.
+__device__ inline void moe_square(uint32_t id, uint32_t rows, uint32_t cols, int* row, int* col) {
+  constexpr uint32_t kBand = 8;
+  const uint32_t band = id / (kBand * cols), in = id % (kBand * cols), high = min(kBand, rows - band * kBand);
   *row = band * kBand + in % high;
   *col = in / high;
 }
 
-// m-tiles there are, the rows of no expert among them
-__device__ inline int64_t moe_count_tiles(const MoeProduct& p, int rows) {
-  if (!p.expert_ptr) return (p.n_rows + rows - 1) / rows;
-  const int lane = threadIdx.x & 63;
-  int sum = 0;
-  for (int e = lane; e <= p.n_experts; e += 64) {
-    const int lo = p.expert_ptr[e], hi = e < p.n_experts ? p.expert_ptr[e + 1] : (int)p.n_rows;
-    sum += (hi - lo + rows - 1) / rows;
-  }
+// The experts' m-tiles, in LDS for as long as a workgroup runs: an expert's rows begin at `row` and its tiles end before
+// `last`; number n_experts are the rows of no expert.  One wavefront fills it in.  Returns the number of m-tiles.
+struct MoeTable {
+  int32_t row[kMoeMaxExperts + 2], last[kMoeMaxExperts + 1];
+};
+__device__ inline uint32_t moe_fill_table(const MoeProduct& p, int rows, MoeTable* table) {
+  if (!p.expert_ptr) return (uint32_t)((p.n_rows + rows - 1) / rows);
+  if (threadIdx.x < 64) {
+    int before = 0;
+    for (int e0 = 0; e0 <= p.n_experts; e0 += 64) {
+      const int e = e0 + (int)threadIdx.x;
+      int lo = (int)p.n_rows, hi = (int)p.n_rows;
+      if (e <= p.n_experts) lo = p.expert_ptr[e];
+      if (e < p.n_experts) hi = p.expert_ptr[e + 1];
+      int sum = (hi - lo + rows - 1) / rows;
 #pragma unroll
-  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-  return __builtin_amdgcn_readfirstlane(sum);
+      for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(sum, d);
+        if ((int)threadIdx.x >= d) sum += o;
+      }
+      if (e <= p.n_experts) {
+        table->row[e] = lo;
+        table->last[e] = before + sum;
+      }
+      before += __shfl(sum, 63);
+    }
+    if (threadIdx.x == 0) table->row[p.n_experts + 1] = (int)p.n_rows;
+  }
+  __syncthreads();
+  return (uint32_t)__builtin_amdgcn_readfirstlane(table->last[p.n_experts]);
+}
+__device__ inline void moe_look_up(const MoeProduct& p, int rows, int tile, const MoeTable* table, MoeTile* out) {
+  if (!p.expert_ptr) {
+    *out = {0, (int64_t)tile * rows, p.n_rows};
+    return;
+  }
+  int e = 0;  // the first whose tiles end behind this one
+  for (int e0 = 0; e0 <= p.n_experts; e0 += 64) {
+    const int at = e0 + (int)(threadIdx.x & 63);
+    const unsigned long long past = __ballot(at <= p.n_experts && table->last[at <= p.n_experts ? at : 0] > tile);
+    if (past) {
+      e = e0 + __ffsll(past) - 1;
+      break;
+    }
+  }
+  const int begin = e > 0 ? table->last[e - 1] : 0, row = table->row[e];
+  *out = {__builtin_amdgcn_readfirstlane(e), __builtin_amdgcn_readfirstlane(row) + (int64_t)(tile - __builtin_amdgcn_readfirstlane(begin)) * rows,
+          __builtin_amdgcn_readfirstlane(table->row[e + 1])};
 }
 
 // ---- eight elements at a time, 16-byte aligned
-template <typename T>
-__device__ inline void read_8(const T* p, float (&v)[8]) {
-  const Pack<T> w = *(const Pack<T>*)p;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = to_float(w.v[i]);
-}
 template <typename T>
 __device__ inline void write_8(T* p, const float (&v)[8]) {
   Pack<T> w;
@@ -49,99 +80,100 @@ __device__ inline void write_8(T* p, const float (&v)[8]) {
   for (int i = 0; i < 8; ++i) w.v[i] = from_float<T>(v[i]);
   *(Pack<T>*)p = w;
 }
-template <int kAct>
+template <int kAct, typename T>
 __device__ inline void act_8(float (&v)[8]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = act_value<kAct>(v[i]);
+  for (int i = 0; i < 8; ++i) v[i] = act_value<kAct, T>(v[i]);
 }
-template <int kAct>
+template <int kAct, typename T>
 __device__ inline void slope_8(float (&v)[8], const float (&z)[8]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = act_slope<kAct>(v[i], z[i]);
+  for (int i = 0; i < 8; ++i) v[i] = act_slope<kAct, T>(v[i], z[i]);
 }
 
-template <typename T, MoeOp kOp>
-__device__ inline void moe_emit_8(const MoeProduct& p, int32_t act, int expert, int64_t i, int32_t j, const float* acc) {
-  float v[8], o[8];
+template <typename T>
+__device__ inline void add_8(float (&v)[8], const Pack<T>& w) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] += to_float(w.v[i]);
+}
+
+// what comes after the sums: nothing, an activation of one column, swiglu's pairs
+enum MoeEnd { kEndNone, kEndAct, kEndSwiglu };
+
+// Eight columns of a row of C from the sums: `bias` and `other` (forward: the residual; dx: z of the product before) have been
+// read by the caller, together for many rows.
+template <typename T, MoeOp kOp, MoeEnd kEnd>
+__device__ inline void moe_emit_8(const MoeProduct& p, int32_t act, int expert, int64_t i, int32_t j, const float* acc, const Pack<T>& bias,
+                                  const Pack<T>& other, const Pack<T>& pair) {
+  float v[8];
 #pragma unroll
   for (int x = 0; x < 8; ++x) v[x] = acc[x];
   if constexpr (kOp == kMoeForward) {
-    if (p.bias) {
-      read_8((const T*)p.bias + expert * p.bias_stride + j, o);
-#pragma unroll
-      for (int x = 0; x < 8; ++x) v[x] += o[x];
-    }
+    add_8(v, bias);
     if (p.pre) write_8((T*)p.pre + i * p.ld_pre + j, v);
-    if (act == SPTIR_ACT_RELU) act_8<SPTIR_ACT_RELU>(v);
-    else if (act == SPTIR_ACT_GELU) act_8<SPTIR_ACT_GELU>(v);
-    else if (act == SPTIR_ACT_SILU) act_8<SPTIR_ACT_SILU>(v);
-    if (p.residual) {
-      read_8((const T*)p.residual + i * p.ld_residual + j, o);
-#pragma unroll
-      for (int x = 0; x < 8; ++x) v[x] += o[x];
+    if constexpr (kEnd == kEndAct) {
+      if (act == SPTIR_ACT_RELU) act_8<SPTIR_ACT_RELU, T>(v);
+      else if (act == SPTIR_ACT_GELU) act_8<SPTIR_ACT_GELU, T>(v);
+      else act_8<SPTIR_ACT_SILU, T>(v);
     }
+    add_8(v, other);
     write_8((T*)p.C + i * p.ldc + j, v);
   } else if constexpr (kOp == kMoeDx) {
-    if (act != SPTIR_ACT_NONE) {
-      const T* z = (const T*)p.pre + i * p.ld_pre + j;
-      read_8(z, o);
-      if (act == SPTIR_ACT_RELU) slope_8<SPTIR_ACT_RELU>(v, o);
-      else if (act == SPTIR_ACT_GELU) slope_8<SPTIR_ACT_GELU>(v, o);
-      else if (act == SPTIR_ACT_SILU) slope_8<SPTIR_ACT_SILU>(v, o);
-      else {
-        float u[8], du[8];
-        read_8(z + p.n_j, u);
+    if constexpr (kEnd == kEndAct) {
+      float z[8];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) act_gated_slope(v[x], o[x], u[x], &v[x], &du[x]);
-        write_8((T*)p.C + i * p.ldc + j + p.n_j, du);
-      }
+      for (int x = 0; x < 8; ++x) z[x] = to_float(other.v[x]);
+      if (act == SPTIR_ACT_RELU) slope_8<SPTIR_ACT_RELU, T>(v, z);
+      else if (act == SPTIR_ACT_GELU) slope_8<SPTIR_ACT_GELU, T>(v, z);
+      else slope_8<SPTIR_ACT_SILU, T>(v, z);
+    } else if constexpr (kEnd == kEndSwiglu) {
+      float du[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) act_gated_slope<T>(v[x], to_float(other.v[x]), to_float(pair.v[x]), &v[x], &du[x]);
+      write_8((T*)p.C + i * p.ldc + j + p.n_j, du);
     }
     write_8((T*)p.C + i * p.ldc + j, v);
   } else {
     write_8((T*)p.C + expert * p.c_stride + i * p.ldc + j, v);
   }
 }
+// swiglu: eight columns of y from the sums of their gates and of what goes with them
 template <typename T>
-__device__ inline void moe_emit_gated_8(const MoeProduct& p, int expert, int64_t i, int32_t j, const float* gate, const float* up) {
-  const int32_t n = p.n_j / 2;
-  float g[8], u[8], o[8];
+__device__ inline void moe_emit_gated_8(const MoeProduct& p, int64_t i, int32_t j, const float* gate, const float* up, const Pack<T>& bias_g,
+                                        const Pack<T>& bias_u, const Pack<T>& residual) {
+  float g[8], u[8];
 #pragma unroll
   for (int x = 0; x < 8; ++x) { g[x] = gate[x]; u[x] = up[x]; }
-  if (p.bias) {
-    const T* b = (const T*)p.bias + expert * p.bias_stride + j;
-    read_8(b, o);
-#pragma unroll
-    for (int x = 0; x < 8; ++x) g[x] += o[x];
-    read_8(b + n, o);
-#pragma unroll
-    for (int x = 0; x < 8; ++x) u[x] += o[x];
-  }
+  add_8(g, bias_g);
+  add_8(u, bias_u);
   if (p.pre) {
     T* z = (T*)p.pre + i * p.ld_pre + j;
     write_8(z, g);
-    write_8(z + n, u);
+    write_8(z + p.n_j / 2, u);
   }
 #pragma unroll
-  for (int x = 0; x < 8; ++x) g[x] = act_gated(g[x], u[x]);
-  if (p.residual) {
-    read_8((const T*)p.residual + i * p.ld_residual + j, o);
-#pragma unroll
-    for (int x = 0; x < 8; ++x) g[x] += o[x];
-  }
+  for (int x = 0; x < 8; ++x) g[x] = act_gated<T>(g[x], u[x]);
+  add_8(g, residual);
   write_8((T*)p.C + i * p.ldc + j, g);
 }
-template <typename T, MoeOp kOp, bool kGated>
-__device__ inline void moe_clear_8(const MoeProduct& p, int32_t act, int64_t i, int32_t j) {
+template <typename T, MoeOp kOp, MoeEnd kEnd>
+__device__ inline void moe_clear_8(const MoeProduct& p, int64_t i, int32_t j) {
   const float zero[8] = {};
   write_8((T*)p.C + i * p.ldc + j, zero);
   if (kOp == kMoeForward && p.pre) {
     write_8((T*)p.pre + i * p.ld_pre + j, zero);
-    if (kGated) write_8((T*)p.pre + i * p.ld_pre + j + p.n_j / 2, zero);
+    if (kEnd == kEndSwiglu) write_8((T*)p.pre + i * p.ld_pre + j + p.n_j / 2, zero);
   }
-  if (kOp == kMoeDx && act == SPTIR_ACT_SWIGLU) write_8((T*)p.C + i * p.ldc + j + p.n_j, zero);
+  if (kOp == kMoeDx && kEnd == kEndSwiglu) write_8((T*)p.C + i * p.ldc + j + p.n_j, zero);
 }
 
-// ---- launches (moe_tiles.hip)
+// the tiles' kernels count 16-byte words of an operand with 32 bits
+inline bool moe_near(int64_t rows, int64_t ld) { return rows == 0 || ld < ((int64_t)1 << 34) / rows; }
+
+// ---- launches (moe_few.hip: any alignment; moe_tiles.hip: 16-byte words)
+double moe_few_estimate(int32_t type, const MoeProduct& p, int32_t* fragments);  // microseconds
+sptir_status_t moe_few_forward(int32_t type, int32_t act, const MoeProduct& p, int32_t fragments, hipStream_t stream);
+double moe_tiles_forward_estimate(int32_t act, const MoeProduct& p);
 sptir_status_t moe_tiles_forward(int32_t type, int32_t act, const MoeProduct& p, hipStream_t stream);
 sptir_status_t moe_tiles_dx(int32_t type, int32_t act, const MoeProduct& p, hipStream_t stream);
 sptir_status_t moe_tiles_dw(int32_t type, const MoeProduct& p, hipStream_t stream);
