@@ -84,11 +84,10 @@ inline int64_t moe_most_tiles(int64_t n_rows, int32_t n_experts, bool routed, in
   return std::min<int64_t>(n_rows, n_rows / rows + n_experts + 1);
 }
 
-__device__ inline int64_t moe_x_row(const MoeProduct& p, int64_t s) {
-  if (!p.entry_of) return s;
-  const uint32_t x = (uint32_t)p.entry_of[s];
-  return p.k_mul ? __umulhi(x, p.k_mul) >> p.k_shift : x;
+__device__ inline int64_t moe_token(const MoeProduct& p, int32_t entry) {
+  return p.k_mul ? __umulhi((uint32_t)entry, p.k_mul) >> p.k_shift : (uint32_t)entry;
 }
+__device__ inline int64_t moe_x_row(const MoeProduct& p, int64_t s) { return p.entry_of ? moe_token(p, p.entry_of[s]) : s; }
 // With 2^(b - 1) < k <= 2^b and m = floor(2^(31 + b) / k) + 1, m k = 2^(31 + b) + d, 0 < d <= k <= 2^b: x m / 2^(31 + b) exceeds
 // x / k by x d / (k 2^(31 + b)) < 1 / k, which moves no quotient of an x < 2^31.  m < 2^32 from k = 2 on; 0 stands for k = 1.
 inline void moe_divide_by(int32_t k, uint32_t* mul, uint32_t* shift) {

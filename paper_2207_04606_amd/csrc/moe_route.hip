@@ -22,62 +22,89 @@ sptir_status_t moe_check_routing(const sptir_moe_routing_t* r) {
 
 namespace {
 
-__device__ inline float wave_max(float v) {
-  for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+// A row of 16 lanes turned by n, without a stop in LDS
+template <int kTurn>
+__device__ inline float turned(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + kTurn, 0xf, 0xf, false));
+}
+// over the L = 16 or 64 lanes of a token
+template <int L, typename F>
+__device__ inline float over_lanes(float v, F&& f) {
+  v = f(v, turned<8>(v));
+  v = f(v, turned<4>(v));
+  v = f(v, turned<2>(v));
+  v = f(v, turned<1>(v));
+  if constexpr (L == 64) {
+    v = f(v, __shfl_xor(v, 16));
+    v = f(v, __shfl_xor(v, 32));
+  }
   return v;
 }
-__device__ inline float wave_sum(float v) {
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+template <int L>
+__device__ inline float lanes_max(float v) {
+  return over_lanes<L>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int L>
+__device__ inline float lanes_sum(float v) {
+  return over_lanes<L>(v, [](float a, float b) { return a + b; });
 }
 
-// A wavefront per token; lane l has the experts l * C .. l * C + C - 1, so that the lowest lane with the largest logit has
-// the lowest id.
+// The logits l * C .. l * C + C - 1 of a token's lane l; -inf past the last.
 template <typename T, int C>
+__device__ inline void read_logits(const T* row, int first, int n_experts, float (&l)[C]) {
+  if (first + C <= n_experts) {  // (any alignment of an element)
+    T v[C];
+    __builtin_memcpy(v, row + first, sizeof(v));
+#pragma unroll
+    for (int c = 0; c < C; ++c) l[c] = to_float(v[c]);
+  } else {
+#pragma unroll
+    for (int c = 0; c < C; ++c) l[c] = first + c < n_experts ? to_float(row[first + c]) : -INFINITY;
+  }
+}
+
+// L lanes per token; lane l has the experts l * C .. l * C + C - 1, so that the lowest lane with the largest logit has the
+// lowest id.  Bound by launch and memory latency: k rounds of C comparisons and four turns of 16 lanes, for four tokens of a
+// wavefront at once (16,384 tokens, 128 experts, 8 choices: 18 us with a wavefront per token and shuffles through LDS).
+template <typename T, int L, int C>
 __global__ __launch_bounds__(256) void k_moe_route(const T* __restrict__ logits, int64_t ld, int32_t n_tokens, int32_t n_experts,
                                                    int32_t top_k, int32_t normalise, int32_t* __restrict__ experts,
                                                    float* __restrict__ weights) {
-  const int lane = threadIdx.x & 63;
-  const int t = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (t >= n_tokens) return;
-  const T* row = logits + (int64_t)t * ld;
+  const int lane = threadIdx.x & (L - 1);
+  const int t = blockIdx.x * (256 / L) + threadIdx.x / L;
+  if (t >= n_tokens) return;  // (whole groups of L lanes)
   float l[C];
+  read_logits<T, C>(logits + (int64_t)t * ld, lane * C, n_experts, l);
   float top = -INFINITY;
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const int e = lane * C + c;
-    l[c] = e < n_experts ? to_float(row[e]) : -INFINITY;
-    top = fmaxf(top, l[c]);  // (not the NaN)
-  }
-  top = wave_max(top);
+  for (int c = 0; c < C; ++c) top = fmaxf(top, l[c]);  // (not the NaN)
+  top = lanes_max<L>(top);
   float all = 0.f;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    if (lane * C + c < n_experts) all += l[c] == -INFINITY ? 0.f : expf(l[c] - top);
+    if (!normalise) all += l[c] == -INFINITY ? 0.f : expf(l[c] - top);
     if (!(l[c] > -INFINITY)) l[c] = -INFINITY;
   }
-  all = wave_sum(all);
   float mine = -INFINITY;  // the choice of this lane's number
   int id = -1;
   for (int j = 0; j < top_k; ++j) {
-    float best = -INFINITY;
+    float best = l[0];
     int at = 0;
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int c = 1; c < C; ++c)
       if (l[c] > best) { best = l[c]; at = c; }
-    const float most = wave_max(best);
-    if (most == -INFINITY) break;
-    const int owner = __ffsll((unsigned long long)__ballot(best == most)) - 1;
-    const int e = __shfl(lane * C + at, owner);
-    if (lane == j) { mine = most; id = e; }
-    if (lane == owner) {
+    const float most = lanes_max<L>(best);
+    const unsigned long long tied = __ballot(best == most) >> ((threadIdx.x & 63) - lane);
+    const int owner = __ffsll(L == 64 ? tied : tied & 0xffff) - 1;
+    // (the owner's expert to all lanes, as a float: below 2^24)
+    const float e = lanes_max<L>(lane == owner ? (float)(lane * C + at) : -1.f);
+    if (lane == j && most > -INFINITY) { mine = most; id = (int)e; }
 #pragma unroll
-      for (int c = 0; c < C; ++c)
-        if (c == at) l[c] = -INFINITY;
-    }
+    for (int c = 0; c < C; ++c)
+      if (lane == owner && c == at) l[c] = -INFINITY;
   }
   float w = id >= 0 ? expf(mine - top) : 0.f;
-  const float total = normalise ? wave_sum(w) : all;
+  const float total = lanes_sum<L>(normalise ? w : all);
   if (id >= 0) w /= total;
   if (lane < top_k) {
     experts[(int64_t)t * top_k + lane] = id;
@@ -85,72 +112,85 @@ __global__ __launch_bounds__(256) void k_moe_route(const T* __restrict__ logits,
   }
 }
 
-// dl[e] = [e chosen] w (dw - mean), mean = sum w dw over the choices; without normalise dl[e] = [e chosen] w dw - p[e] mean
-template <typename T, int C>
+// dl[e] = w (dw - mean) for a choice, mean = sum w dw over the choices; for others 0, or without normalise -p[e] mean
+template <typename T, int L, int C>
 __global__ __launch_bounds__(256) void k_moe_route_backward(const T* __restrict__ logits, int64_t ld, int32_t n_tokens,
                                                             int32_t n_experts, int32_t top_k, int32_t normalise,
                                                             const int32_t* __restrict__ experts,
                                                             const float* __restrict__ weights,
                                                             const float* __restrict__ d_weights, T* __restrict__ d_logits,
                                                             int64_t ld_d) {
-  const int lane = threadIdx.x & 63;
-  const int t = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & (L - 1);
+  const int t = blockIdx.x * (256 / L) + threadIdx.x / L;
   if (t >= n_tokens) return;
   int id = -1;
   float w = 0.f, dw = 0.f;
   if (lane < top_k) {
-    id = experts[(int64_t)t * top_k + lane];
-    if (id >= 0) {
-      w = weights[(int64_t)t * top_k + lane];
-      dw = d_weights[(int64_t)t * top_k + lane];
-    }
+    const int64_t i = (int64_t)t * top_k + lane;
+    id = experts[i];
+    w = weights[i];
+    dw = d_weights[i];
+    if (id < 0) w = dw = 0.f;
   }
-  const float mean = wave_sum(w * dw);
+  const float mean = lanes_sum<L>(w * dw);
   float d[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) d[c] = 0.f;
   if (!normalise) {
-    const T* row = logits + (int64_t)t * ld;
     float l[C], top = -INFINITY, all = 0.f;
+    read_logits<T, C>(logits + (int64_t)t * ld, lane * C, n_experts, l);
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int e = lane * C + c;
-      l[c] = e < n_experts ? to_float(row[e]) : -INFINITY;
-      top = fmaxf(top, l[c]);
-    }
-    top = wave_max(top);
+    for (int c = 0; c < C; ++c) top = fmaxf(top, l[c]);
+    top = lanes_max<L>(top);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       l[c] = l[c] == -INFINITY ? 0.f : expf(l[c] - top);
       all += l[c];
     }
-    all = wave_sum(all);
+    all = lanes_sum<L>(all);
     if (all != 0.f) {  // (a token without any choice: 0)
 #pragma unroll
       for (int c = 0; c < C; ++c) d[c] = -(l[c] / all) * mean;
     }
   }
-  const float of_choice = normalise ? w * (dw - mean) : w * dw;
+  const float of_choice = w * (dw - mean);
   for (int j = 0; j < top_k; ++j) {
-    const int e = __shfl(id, j);
-    const float g = __shfl(of_choice, j);
+    const int e = __shfl(id, j, L);
+    const float g = __shfl(of_choice, j, L);
 #pragma unroll
     for (int c = 0; c < C; ++c)
-      if (e == lane * C + c) d[c] += g;
+      if (e == lane * C + c) d[c] = g;
   }
-  T* out = d_logits + (int64_t)t * ld_d;
+  T* out = d_logits + (int64_t)t * ld_d + lane * C;
+  if (lane * C + C <= n_experts) {
+    T v[C];
 #pragma unroll
-  for (int c = 0; c < C; ++c)
-    if (lane * C + c < n_experts) out[lane * C + c] = from_float<T>(d[c]);
+    for (int c = 0; c < C; ++c) v[c] = from_float<T>(d[c]);
+    __builtin_memcpy(out, v, sizeof(v));
+  } else {
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (lane * C + c < n_experts) out[c] = from_float<T>(d[c]);
+  }
 }
 
+// 16 lanes per token where its experts and choices fit them
 template <typename F>
-void with_columns(int32_t n_experts, F&& f) {
-  if (n_experts <= 64) f(std::integral_constant<int, 1>{});
-  else if (n_experts <= 128) f(std::integral_constant<int, 2>{});
-  else if (n_experts <= 256) f(std::integral_constant<int, 4>{});
-  else if (n_experts <= 512) f(std::integral_constant<int, 8>{});
-  else f(std::integral_constant<int, 16>{});
+void with_lanes(int32_t n_experts, int32_t top_k, F&& f) {
+  using std::integral_constant;
+  if (top_k <= 16 && n_experts <= 256) {
+    const integral_constant<int, 16> lanes;
+    if (n_experts <= 16) f(lanes, integral_constant<int, 1>{});
+    else if (n_experts <= 32) f(lanes, integral_constant<int, 2>{});
+    else if (n_experts <= 64) f(lanes, integral_constant<int, 4>{});
+    else if (n_experts <= 128) f(lanes, integral_constant<int, 8>{});
+    else f(lanes, integral_constant<int, 16>{});
+  } else {
+    const integral_constant<int, 64> lanes;
+    if (n_experts <= 256) f(lanes, integral_constant<int, 4>{});
+    else if (n_experts <= 512) f(lanes, integral_constant<int, 8>{});
+    else f(lanes, integral_constant<int, 16>{});
+  }
 }
 
 // ------------------------------------------------------------------- sort by expert
@@ -181,41 +221,56 @@ __global__ __launch_bounds__(1024) void k_moe_count(const int32_t* __restrict__ 
   for (int e = threadIdx.x; e < n_experts; e += blockDim.x) counts[(int64_t)blockIdx.x * n_experts + e] = count[e];
 }
 
+constexpr int kHeld = 16;  // turns of 64 entries that a wavefront holds: 16 K entries of a workgroup are read once
 __global__ __launch_bounds__(1024) void k_moe_place(const int32_t* __restrict__ experts, int64_t n, int64_t part, int32_t n_experts,
                                                     const int32_t* __restrict__ counts, int32_t* __restrict__ expert_ptr,
                                                     int32_t* __restrict__ entry_of, int32_t* __restrict__ slot_of) {
-  extern __shared__ int32_t place[];  // [waves][n_experts], then the expert's total, [n_experts]
+  extern __shared__ int32_t place[];  // [waves][n_experts], then the experts' totals and what other workgroups have before, [n_experts] each
   __shared__ int32_t wave_total[16];
   const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   int32_t* mine = place + wave * n_experts;
-  int32_t* total = place + waves * n_experts;
-  for (int i = threadIdx.x; i < waves * n_experts; i += blockDim.x) place[i] = 0;
-  __syncthreads();
+  int32_t *total = place + waves * n_experts, *before = total + n_experts;
   const int64_t lo = blockIdx.x * part, hi = min(n, lo + part);
   const int64_t seg = ((hi - lo + waves - 1) / waves + 63) / 64 * 64;
   const int64_t w_lo = lo + wave * seg, w_hi = min(hi, w_lo + seg);
-  for (int64_t i = w_lo + lane; i < w_hi; i += 64) {
-    const int e = experts[i];
-    if (e >= 0 && e < n_experts) atomicAdd(&mine[e], 1);
-  }
+  // an entry's expert, n_experts for one that is dropped
+  auto expert_at = [&](int64_t i) {
+    const int e = i < w_hi ? experts[i] : -1;
+    return e >= 0 && e < n_experts ? e : n_experts;
+  };
+  int held[kHeld];
+#pragma unroll
+  for (int h = 0; h < kHeld; ++h) held[h] = w_lo + 64 * h < w_hi ? expert_at(w_lo + 64 * h + lane) : n_experts;
+  for (int i = threadIdx.x; i < (waves + 2) * n_experts; i += blockDim.x) place[i] = 0;
   __syncthreads();
-  // an expert's first places inside the workgroup, and its total over all workgroups
-  for (int e = threadIdx.x; e < n_experts; e += blockDim.x) {
-    int before = 0, all = 0;
-    if (counts) {
-      for (int g = 0; g < (int)gridDim.x; ++g) {
-        const int c = counts[(int64_t)g * n_experts + e];
-        if (g < (int)blockIdx.x) before += c;
-        all += c;
+#pragma unroll
+  for (int h = 0; h < kHeld; ++h)
+    if (held[h] < n_experts) atomicAdd(&mine[held[h]], 1);
+  for (int64_t i = w_lo + 64 * kHeld + lane; i < w_hi; i += 64) {
+    const int e = expert_at(i);
+    if (e < n_experts) atomicAdd(&mine[e], 1);
+  }
+  if (counts) {  // (whole numbers: the order of these sums changes nothing)
+    const int many = (int)gridDim.x * n_experts, own = (int)blockIdx.x * n_experts;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < many; i += blockDim.x) {
+      const int c = counts[i];
+      if (c) {
+        atomicAdd(&total[i % n_experts], c);
+        if (i < own) atomicAdd(&before[i % n_experts], c);
       }
     }
-    int at = before;
+  }
+  __syncthreads();
+  // an expert's first places inside the workgroup, and without other workgroups its total
+  for (int e = threadIdx.x; e < n_experts; e += blockDim.x) {
+    int at = before[e];
     for (int w = 0; w < waves; ++w) {
       const int c = place[w * n_experts + e];
       place[w * n_experts + e] = at;
       at += c;
     }
-    total[e] = counts ? all : at;
+    if (!counts) total[e] = at;
   }
   __syncthreads();
   // exclusive scan of the totals; kMoeMaxExperts = 1024 may be more than the workgroup has threads
@@ -235,24 +290,16 @@ __global__ __launch_bounds__(1024) void k_moe_place(const int32_t* __restrict__ 
       if (w < wave) base += wave_total[w];
       running += wave_total[w];
     }
-    if (e < n_experts) total[e] = base + s - c;
+    if (e < n_experts) {
+      const int first = base + s - c;
+      if (blockIdx.x == 0) expert_ptr[e] = first;
+      for (int w = 0; w < waves; ++w) place[w * n_experts + e] += first;
+    }
     __syncthreads();
   }
-  for (int e = threadIdx.x; e < n_experts; e += blockDim.x) {
-    const int first = total[e];
-    if (blockIdx.x == 0) expert_ptr[e] = first;
-    for (int w = 0; w < waves; ++w) place[w * n_experts + e] += first;
-  }
   if (blockIdx.x == 0 && threadIdx.x == 0) expert_ptr[n_experts] = running;
-  __syncthreads();
   const int bits = 32 - __clz(n_experts);  // (n_experts itself stands for "dropped")
-  for (int64_t i0 = w_lo; i0 < w_hi; i0 += 64) {
-    const int64_t i = i0 + lane;
-    int e = n_experts;
-    if (i < w_hi) {
-      const int given = experts[i];
-      if (given >= 0 && given < n_experts) e = given;
-    }
+  auto put = [&](int64_t i, int e) {
     const unsigned long long same = lanes_alike(e, bits);
     const int rank = __popcll(same & ((1ull << lane) - 1));
     int slot = -1;
@@ -264,7 +311,11 @@ __global__ __launch_bounds__(1024) void k_moe_place(const int32_t* __restrict__ 
       slot_of[i] = slot;
       if (slot >= 0) entry_of[slot] = (int32_t)i;
     }
-  }
+  };
+#pragma unroll
+  for (int h = 0; h < kHeld; ++h)
+    if (w_lo + 64 * h < w_hi) put(w_lo + 64 * h + lane, held[h]);
+  for (int64_t i0 = w_lo + 64 * kHeld; i0 < w_hi; i0 += 64) put(i0 + lane, expert_at(i0 + lane));
   for (int64_t s = running + (int64_t)blockIdx.x * blockDim.x + threadIdx.x; s < n; s += (int64_t)gridDim.x * blockDim.x)
     entry_of[s] = -1;
 }
@@ -290,11 +341,12 @@ extern "C" sptir_status_t sptir_moe_route(const void* logits, int32_t type, int6
   if (top_k > n_experts || ld_logits < n_experts) return SPTIR_ERR_INVALID_ARG;
   if (n_tokens == 0) return SPTIR_OK;
   if (!logits || !experts || !weights) return SPTIR_ERR_INVALID_ARG;
-  const dim3 grid((n_tokens + 3) / 4);
   moe_with_type(type, [&](auto v) {
     using T = decltype(v);
-    with_columns(n_experts, [&](auto c) {
-      hipLaunchKernelGGL((k_moe_route<T, decltype(c)::value>), grid, dim3(256), 0, (hipStream_t)stream, (const T*)logits, ld_logits,
+    with_lanes(n_experts, top_k, [&](auto l, auto c) {
+      constexpr int kLanes = decltype(l)::value, kTokens = 256 / kLanes;
+      const dim3 grid((n_tokens + kTokens - 1) / kTokens);
+      hipLaunchKernelGGL((k_moe_route<T, kLanes, decltype(c)::value>), grid, dim3(256), 0, (hipStream_t)stream, (const T*)logits, ld_logits,
                          n_tokens, n_experts, top_k, normalise, experts, weights);
     });
   });
@@ -312,11 +364,12 @@ extern "C" sptir_status_t sptir_moe_route_backward(const void* logits, int32_t t
   if (top_k > n_experts || ld_logits < n_experts || ld_d_logits < n_experts) return SPTIR_ERR_INVALID_ARG;
   if (n_tokens == 0) return SPTIR_OK;
   if (!logits || !experts || !weights || !d_weights || !d_logits || d_logits == logits) return SPTIR_ERR_INVALID_ARG;
-  const dim3 grid((n_tokens + 3) / 4);
   moe_with_type(type, [&](auto v) {
     using T = decltype(v);
-    with_columns(n_experts, [&](auto c) {
-      hipLaunchKernelGGL((k_moe_route_backward<T, decltype(c)::value>), grid, dim3(256), 0, (hipStream_t)stream, (const T*)logits,
+    with_lanes(n_experts, top_k, [&](auto l, auto c) {
+      constexpr int kLanes = decltype(l)::value, kTokens = 256 / kLanes;
+      const dim3 grid((n_tokens + kTokens - 1) / kTokens);
+      hipLaunchKernelGGL((k_moe_route_backward<T, kLanes, decltype(c)::value>), grid, dim3(256), 0, (hipStream_t)stream, (const T*)logits,
                          ld_logits, n_tokens, n_experts, top_k, normalise, experts, weights, d_weights, (T*)d_logits, ld_d_logits);
     });
   });
@@ -347,7 +400,7 @@ extern "C" sptir_status_t sptir_moe_sort(const int32_t* experts, int32_t n_token
     hipLaunchKernelGGL(k_moe_count, dim3(groups), dim3(1024), n_experts * sizeof(int32_t), (hipStream_t)stream, experts, n, part,
                        n_experts, (int32_t*)workspace);
   static OncePerDevice allowed;
-  const size_t lds = (size_t)(waves + 1) * n_experts * sizeof(int32_t);
+  const size_t lds = (size_t)(waves + 2) * n_experts * sizeof(int32_t);
   allow_dynamic_lds((const void*)k_moe_place, lds, allowed);
   hipLaunchKernelGGL(k_moe_place, dim3(groups), dim3(64 * waves), lds, (hipStream_t)stream, experts, n, part, n_experts,
                      groups > 1 ? (const int32_t*)workspace : nullptr, expert_ptr, entry_of, slot_of);

@@ -1,5 +1,6 @@
 // Tokens into the order of the experts and back, with the router's weights, and the gradients: copies and short sums, bound
-// by memory.  A wavefront per token: a row of X (or of a gradient) is read once for all the places it goes to.
+// by memory.  A group of lanes per token: a row of X (or of a gradient) is read once for all the places it goes to, and the
+// rows of up to eight choices are on their way at once.
 #include <algorithm>
 
 #include "moe.h"
@@ -7,36 +8,51 @@
 namespace sptir {
 namespace {
 
-// V elements of a row, 16 bytes where V > 1
-template <typename T, int V>
-struct Span { float v[V]; };
-template <typename T, int V>
-__device__ inline Span<T, V> load_span(const T* p) {
-  Span<T, V> s;
-  if constexpr (V == 1) {
-    s.v[0] = to_float(*p);
-  } else {
-    const Pack<T> w = *(const Pack<T>*)p;
+constexpr int kAtOnce = 8;  // choices whose places a lane holds
+
+// A lane's 16 bytes of a row from element c on.  Odd widths and strides are read in the same words as others: where the row
+// ends inside a word the row's last 16 bytes are read, and moved to their place when they have come (loads without branches,
+// so that many are under way at once).  kTiny: the row has no 16 bytes.
+template <typename T>
+struct Span {
+  static constexpr int kN = 16 / sizeof(T);
+  float v[kN];
+};
+template <typename T, bool kTiny>
+__device__ inline u32x4 load_word(const T* row, int c, int width) {
+  if constexpr (kTiny) return read_elements(row + c, width - c);
+  u32x4 w;
+  __builtin_memcpy(&w, row + min(c, width - Span<T>::kN), 16);
+  return w;
+}
+template <typename T, bool kTiny>
+__device__ inline Span<T> spread(u32x4 w, int c, int width) {
+  constexpr int kN = Span<T>::kN;
+  if (!kTiny && width % kN) w = without_first(w, max(c + kN - width, 0) * (int)sizeof(T));
+  T v[kN];
+  __builtin_memcpy(v, &w, 16);
+  Span<T> s;
 #pragma unroll
-    for (int i = 0; i < V; ++i) s.v[i] = to_float(w.v[i]);
-  }
+  for (int i = 0; i < kN; ++i) s.v[i] = to_float(v[i]);
   return s;
 }
-template <typename T, int V>
-__device__ inline void store_span(T* p, const Span<T, V>& s) {
-  if constexpr (V == 1) {
-    *p = from_float<T>(s.v[0]);
-  } else {
-    Pack<T> w;
+template <typename T, bool kTiny>
+__device__ inline Span<T> load_span(const T* row, int c, int width) { return spread<T, kTiny>(load_word<T, kTiny>(row, c, width), c, width); }
+template <typename T>
+__device__ inline void store_span(T* p, int many, const Span<T>& s) {
+  constexpr int kN = Span<T>::kN;
+  T v[kN];
 #pragma unroll
-    for (int i = 0; i < V; ++i) w.v[i] = from_float<T>(s.v[i]);
-    *(Pack<T>*)p = w;
-  }
+  for (int i = 0; i < kN; ++i) v[i] = from_float<T>(s.v[i]);
+  u32x4 w;
+  __builtin_memcpy(&w, v, 16);
+  write_word(p, w, many);
 }
 
 struct RowArgs {
   sptir_moe_routing_t r;
   int32_t width;
+  int32_t lanes;       // of a token: a power of two up to 64
   const void *a, *b;   // gather: X; combine: Ys, residual; backward: dY, Ys
   int64_t lda, ldb;
   const float* weights;
@@ -45,114 +61,180 @@ struct RowArgs {
   float* d_weights;
 };
 
+// this lane's place: its token's number among all groups of lanes, their number, its place in the group
+struct Place {
+  int64_t group, groups;
+  int lane;
+};
+__device__ inline Place place_of(const RowArgs& p) {
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  return {id / p.lanes, (int64_t)gridDim.x * 256 / p.lanes, (int)(id & (p.lanes - 1))};
+}
+
+// the places and weights of choices j0 .. j0 + kAtOnce - 1 of token t; -1 where there is none
+struct Choices {
+  int slot[kAtOnce];
+  float weight[kAtOnce];
+};
+__device__ inline Choices read_choices(const RowArgs& p, int64_t t, int j0) {
+  Choices c;
+#pragma unroll
+  for (int x = 0; x < kAtOnce; ++x) {
+    const bool there = j0 + x < p.r.top_k;
+    const int64_t i = t * p.r.top_k + j0 + x;
+    c.slot[x] = there ? p.r.slot_of[i] : -1;
+    c.weight[x] = there && p.weights ? p.weights[i] : 1.f;
+  }
+  return c;
+}
+
 // zeros in the sorted rows that belong to no entry
-template <typename T, int V>
-__device__ inline void clear_tail(const RowArgs& p, int wave, int n_waves, int lane) {
+template <typename T>
+__device__ inline void clear_tail(const RowArgs& p, const Place& me) {
+  constexpr int kN = Span<T>::kN;
   const int64_t n = (int64_t)p.r.n_tokens * p.r.top_k;
-  Span<T, V> zero;
-#pragma unroll
-  for (int i = 0; i < V; ++i) zero.v[i] = 0.f;
-  for (int64_t s = p.r.expert_ptr[p.r.n_experts] + (int64_t)wave; s < n; s += n_waves)
-    for (int c = lane * V; c < p.width; c += 64 * V) store_span<T, V>((T*)p.out + s * p.ldo + c, zero);
+  const Span<T> zero = {};
+  for (int64_t s = p.r.expert_ptr[p.r.n_experts] + me.group; s < n; s += me.groups)
+    for (int c = me.lane * kN; c < p.width; c += p.lanes * kN) store_span<T>((T*)p.out + s * p.ldo + c, p.width - c, zero);
 }
 
-template <typename T, int V>
+template <typename T, bool kTiny>
 __global__ __launch_bounds__(256) void k_moe_gather(RowArgs p) {
-  const int lane = threadIdx.x & 63, wave = blockIdx.x * 4 + (threadIdx.x >> 6), n_waves = gridDim.x * 4;
-  const int k = p.r.top_k;
-  for (int t = wave; t < p.r.n_tokens; t += n_waves) {
-    const T* x = (const T*)p.a + (int64_t)t * p.lda;
-    for (int c = lane * V; c < p.width; c += 64 * V) {
-      const Span<T, V> v = load_span<T, V>(x + c);
-      for (int j = 0; j < k; ++j) {
-        const int64_t i = (int64_t)t * k + j;
-        const int s = p.r.slot_of[i];
-        if (s < 0) continue;
-        Span<T, V> o = v;
+  constexpr int kN = Span<T>::kN;
+  const Place me = place_of(p);
+  for (int64_t t = me.group; t < p.r.n_tokens; t += me.groups) {
+    for (int j0 = 0; j0 < p.r.top_k; j0 += kAtOnce) {
+      const Choices to = read_choices(p, t, j0);
+      for (int c = me.lane * kN; c < p.width; c += p.lanes * kN) {
+        u32x4 word = load_word<T, kTiny>((const T*)p.a + t * p.lda, c, p.width);
         if (p.weights) {
-          const float w = p.weights[i];
+          const Span<T> v = spread<T, kTiny>(word, c, p.width);
 #pragma unroll
-          for (int q = 0; q < V; ++q) o.v[q] *= w;
+          for (int x = 0; x < kAtOnce; ++x) {
+            if (to.slot[x] < 0) continue;
+            Span<T> o;
+#pragma unroll
+            for (int i = 0; i < kN; ++i) o.v[i] = v.v[i] * to.weight[x];
+            store_span<T>((T*)p.out + to.slot[x] * p.ldo + c, p.width - c, o);
+          }
+        } else {
+          if (!kTiny && p.width % kN) word = without_first(word, max(c + kN - p.width, 0) * (int)sizeof(T));
+#pragma unroll
+          for (int x = 0; x < kAtOnce; ++x)
+            if (to.slot[x] >= 0) write_word((T*)p.out + to.slot[x] * p.ldo + c, word, p.width - c);
         }
-        store_span<T, V>((T*)p.out + (int64_t)s * p.ldo + c, o);
       }
     }
   }
-  clear_tail<T, V>(p, wave, n_waves, lane);
+  clear_tail<T>(p, me);
 }
 
-template <typename T, int V>
+// Rows of no entry are read at row 0 instead, so that all loads are under way before the first is waited for, and not added.
+template <typename T, bool kTiny>
 __global__ __launch_bounds__(256) void k_moe_combine(RowArgs p) {
-  const int lane = threadIdx.x & 63, wave = blockIdx.x * 4 + (threadIdx.x >> 6), n_waves = gridDim.x * 4;
-  const int k = p.r.top_k;
-  for (int t = wave; t < p.r.n_tokens; t += n_waves) {
-    for (int c = lane * V; c < p.width; c += 64 * V) {
-      Span<T, V> sum;
+  constexpr int kN = Span<T>::kN;
+  const Place me = place_of(p);
+  for (int64_t t = me.group; t < p.r.n_tokens; t += me.groups) {
+    Choices from = read_choices(p, t, 0);
+    for (int c = me.lane * kN; c < p.width; c += p.lanes * kN) {
+      const int many = p.width - c;
+      Span<T> sum = {};
+      if (p.b) sum = load_span<T, kTiny>((const T*)p.b + t * p.ldb, c, p.width);
+      for (int j0 = 0; j0 < p.r.top_k; j0 += kAtOnce) {
+        if (p.r.top_k > kAtOnce) from = read_choices(p, t, j0);
+        auto add = [&](auto n) {
+          constexpr int kRows = decltype(n)::value;
+          u32x4 y[kRows];
 #pragma unroll
-      for (int q = 0; q < V; ++q) sum.v[q] = 0.f;
-      if (p.b) sum = load_span<T, V>((const T*)p.b + (int64_t)t * p.ldb + c);
-      for (int j = 0; j < k; ++j) {
-        const int64_t i = (int64_t)t * k + j;
-        const int s = p.r.slot_of[i];
-        if (s < 0) continue;
-        const float w = p.weights ? p.weights[i] : 1.f;
-        const Span<T, V> y = load_span<T, V>((const T*)p.a + (int64_t)s * p.lda + c);
+          for (int x = 0; x < kRows; ++x) y[x] = load_word<T, kTiny>((const T*)p.a + max(from.slot[x], 0) * p.lda, c, p.width);
 #pragma unroll
-        for (int q = 0; q < V; ++q) sum.v[q] = fmaf(w, y.v[q], sum.v[q]);
+          for (int x = 0; x < kRows; ++x) {
+            const Span<T> row = spread<T, kTiny>(y[x], c, p.width);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) sum.v[i] = from.slot[x] >= 0 ? fmaf(from.weight[x], row.v[i], sum.v[i]) : sum.v[i];
+          }
+        };
+        const int left = p.r.top_k - j0;
+        if (left <= 1) add(std::integral_constant<int, 1>{});
+        else if (left <= 2) add(std::integral_constant<int, 2>{});
+        else if (left <= 4) add(std::integral_constant<int, 4>{});
+        else add(std::integral_constant<int, 8>{});
       }
-      store_span<T, V>((T*)p.out + (int64_t)t * p.ldo + c, sum);
+      store_span<T>((T*)p.out + t * p.ldo + c, many, sum);
     }
   }
 }
 
-template <typename T, int V>
+template <typename T, bool kTiny>
 __global__ __launch_bounds__(256) void k_moe_combine_backward(RowArgs p) {
-  const int lane = threadIdx.x & 63, wave = blockIdx.x * 4 + (threadIdx.x >> 6), n_waves = gridDim.x * 4;
-  const int k = p.r.top_k;
-  for (int t = wave; t < p.r.n_tokens; t += n_waves) {
-    const T* dy = (const T*)p.a + (int64_t)t * p.lda;
-    for (int j = 0; j < k; ++j) {
-      const int64_t i = (int64_t)t * k + j;
-      const int s = p.r.slot_of[i];
-      float dot = 0.f;
-      if (s >= 0) {
-        const float w = p.weights ? p.weights[i] : 1.f;
-        for (int c = lane * V; c < p.width; c += 64 * V) {
-          const Span<T, V> d = load_span<T, V>(dy + c);
-          Span<T, V> o;
-#pragma unroll
-          for (int q = 0; q < V; ++q) o.v[q] = w * d.v[q];
-          store_span<T, V>((T*)p.out + (int64_t)s * p.ldo + c, o);
+  constexpr int kN = Span<T>::kN;
+  const Place me = place_of(p);
+  for (int64_t t = me.group; t < p.r.n_tokens; t += me.groups) {
+    for (int j0 = 0; j0 < p.r.top_k; j0 += kAtOnce) {
+      const Choices at = read_choices(p, t, j0);
+      float dot[kAtOnce] = {};
+      auto rows = [&](auto n) {
+        constexpr int kRows = decltype(n)::value;
+        for (int c = me.lane * kN; c < p.width; c += p.lanes * kN) {
+          const int many = p.width - c;
+          const u32x4 word = load_word<T, kTiny>((const T*)p.a + t * p.lda, c, p.width);
+          u32x4 y[kRows] = {};
           if (p.d_weights) {
-            const Span<T, V> y = load_span<T, V>((const T*)p.b + (int64_t)s * p.ldb + c);
 #pragma unroll
-            for (int q = 0; q < V; ++q) dot = fmaf(d.v[q], y.v[q], dot);
+            for (int x = 0; x < kRows; ++x) y[x] = load_word<T, kTiny>((const T*)p.b + max(at.slot[x], 0) * p.ldb, c, p.width);
+          }
+          const Span<T> d = spread<T, kTiny>(word, c, p.width);
+#pragma unroll
+          for (int x = 0; x < kRows; ++x) {
+            const Span<T> row = spread<T, kTiny>(y[x], c, p.width);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) dot[x] = fmaf(d.v[i], row.v[i], dot[x]);
+            if (at.slot[x] < 0) continue;
+            Span<T> o;
+#pragma unroll
+            for (int i = 0; i < kN; ++i) o.v[i] = at.weight[x] * d.v[i];
+            store_span<T>((T*)p.out + at.slot[x] * p.ldo + c, many, o);
           }
         }
-      }
+      };
+      const int left = p.r.top_k - j0;
+      if (left <= 1) rows(std::integral_constant<int, 1>{});
+      else if (left <= 2) rows(std::integral_constant<int, 2>{});
+      else if (left <= 4) rows(std::integral_constant<int, 4>{});
+      else rows(std::integral_constant<int, 8>{});
       if (p.d_weights) {
-        for (int d = 32; d; d >>= 1) dot += __shfl_xor(dot, d);
-        if (lane == 0) p.d_weights[i] = dot;
+#pragma unroll
+        for (int x = 0; x < kAtOnce; ++x) {
+          if (x >= left) continue;
+          float sum = dot[x];
+          for (int d = p.lanes / 2; d; d >>= 1) sum += __shfl_xor(sum, d);
+          if (me.lane == 0) p.d_weights[t * p.r.top_k + j0 + x] = at.slot[x] >= 0 ? sum : 0.f;
+        }
       }
     }
   }
-  clear_tail<T, V>(p, wave, n_waves, lane);
+  clear_tail<T>(p, me);
 }
 
 enum RowsKind { kGather, kCombine, kBackward };
 
-sptir_status_t launch_rows(RowsKind kind, int32_t type, bool words, const RowArgs& p, void* stream) {
-  const dim3 grid((unsigned)std::min<int64_t>(((int64_t)p.r.n_tokens + 3) / 4, 8192));
+sptir_status_t launch_rows(RowsKind kind, int32_t type, RowArgs p, void* stream) {
+  // as many lanes as a row has words, 8 at the least
+  const int per = 16 / moe_type_bytes(type);
+  p.lanes = 8;
+  while (p.lanes < 64 && (int64_t)p.lanes * per < p.width) p.lanes *= 2;
+  const int64_t groups = 256 / p.lanes;
+  const dim3 grid((unsigned)std::min<int64_t>((p.r.n_tokens + groups - 1) / groups, 16384));
   moe_with_type(type, [&](auto v) {
     using T = decltype(v);
-    auto go = [&](auto vec) {
-      constexpr int V = decltype(vec)::value;
-      if (kind == kGather) hipLaunchKernelGGL((k_moe_gather<T, V>), grid, dim3(256), 0, (hipStream_t)stream, p);
-      else if (kind == kCombine) hipLaunchKernelGGL((k_moe_combine<T, V>), grid, dim3(256), 0, (hipStream_t)stream, p);
-      else hipLaunchKernelGGL((k_moe_combine_backward<T, V>), grid, dim3(256), 0, (hipStream_t)stream, p);
+    auto go = [&](auto tiny) {
+      constexpr bool kTiny = decltype(tiny)::value;
+      if (kind == kGather) hipLaunchKernelGGL((k_moe_gather<T, kTiny>), grid, dim3(256), 0, (hipStream_t)stream, p);
+      else if (kind == kCombine) hipLaunchKernelGGL((k_moe_combine<T, kTiny>), grid, dim3(256), 0, (hipStream_t)stream, p);
+      else hipLaunchKernelGGL((k_moe_combine_backward<T, kTiny>), grid, dim3(256), 0, (hipStream_t)stream, p);
     };
-    if (words) go(std::integral_constant<int, Pack<T>::kN>{});
-    else go(std::integral_constant<int, 1>{});
+    if (p.width < per) go(std::true_type{});
+    else go(std::false_type{});
   });
   SPTIR_HIP(hipGetLastError());
   return SPTIR_OK;
@@ -161,6 +243,7 @@ sptir_status_t launch_rows(RowsKind kind, int32_t type, bool words, const RowArg
 // sizes of a call; *empty: there is nothing to do
 sptir_status_t check_rows(const sptir_moe_routing_t* routing, int32_t type, int32_t width, bool* empty) {
   if (!routing || !moe_type_ok(type) || width < 0) return SPTIR_ERR_INVALID_ARG;
+  if (width > INT32_MAX / 2) return SPTIR_ERR_OVERFLOW;
   *empty = routing->n_tokens == 0 || width == 0;
   return moe_check_routing(routing);
 }
@@ -178,8 +261,7 @@ extern "C" sptir_status_t sptir_moe_gather(const sptir_moe_routing_t* routing, i
   if (ldx < width || ldxs < width) return SPTIR_ERR_INVALID_ARG;
   if (empty) return SPTIR_OK;
   if (!X || !Xs || X == Xs) return SPTIR_ERR_INVALID_ARG;
-  const RowArgs p = {*routing, width, X, nullptr, ldx, 0, weights, Xs, ldxs, nullptr};
-  return launch_rows(kGather, type, moe_words(type, width, {X, Xs}, {ldx, ldxs}), p, stream);
+  return launch_rows(kGather, type, {*routing, width, 0, X, nullptr, ldx, 0, weights, Xs, ldxs, nullptr}, stream);
 }
 
 extern "C" sptir_status_t sptir_moe_combine(const sptir_moe_routing_t* routing, int32_t type, int32_t width, const void* Ys,
@@ -191,8 +273,7 @@ extern "C" sptir_status_t sptir_moe_combine(const sptir_moe_routing_t* routing, 
   if (ldys < width || ldy < width || (residual && ld_residual < width)) return SPTIR_ERR_INVALID_ARG;
   if (empty) return SPTIR_OK;
   if (!Ys || !Y || Ys == Y || (residual == Y && ld_residual != ldy)) return SPTIR_ERR_INVALID_ARG;
-  const RowArgs p = {*routing, width, Ys, residual, ldys, ld_residual, weights, Y, ldy, nullptr};
-  return launch_rows(kCombine, type, moe_words(type, width, {Ys, residual, Y}, {ldys, residual ? ld_residual : 0, ldy}), p, stream);
+  return launch_rows(kCombine, type, {*routing, width, 0, Ys, residual, ldys, ld_residual, weights, Y, ldy, nullptr}, stream);
 }
 
 extern "C" sptir_status_t sptir_moe_combine_backward(const sptir_moe_routing_t* routing, int32_t type, int32_t width, const void* dY,
@@ -204,6 +285,5 @@ extern "C" sptir_status_t sptir_moe_combine_backward(const sptir_moe_routing_t* 
   if (ld_dy < width || ld_dys < width || (d_weights && ldys < width)) return SPTIR_ERR_INVALID_ARG;
   if (routing->n_tokens == 0) return SPTIR_OK;
   if (width > 0 && (!dY || !dYs || dY == dYs || (d_weights && (!Ys || Ys == dYs)))) return SPTIR_ERR_INVALID_ARG;
-  const RowArgs p = {*routing, width, dY, d_weights ? Ys : nullptr, ld_dy, ldys, weights, dYs, ld_dys, d_weights};
-  return launch_rows(kBackward, type, moe_words(type, width, {dY, p.b, dYs}, {ld_dy, d_weights ? ldys : 0, ld_dys}), p, stream);
+  return launch_rows(kBackward, type, {*routing, width, 0, dY, Ys, ld_dy, ldys, weights, dYs, ld_dys, d_weights}, stream);
 }

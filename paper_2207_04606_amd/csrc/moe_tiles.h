@@ -72,13 +72,48 @@ __device__ inline void moe_look_up(const MoeProduct& p, int rows, int tile, cons
           __builtin_amdgcn_readfirstlane(table->row[e + 1])};
 }
 
-// ---- eight elements at a time, 16-byte aligned
+// ---- eight elements at a time, of which there are `many`; kWords: they lie in 16-byte words, and whole words of them are there
 template <typename T>
-__device__ inline void write_8(T* p, const float (&v)[8]) {
-  Pack<T> w;
+struct Eight {
+  static constexpr int kN = Pack<T>::kN;
+  typename Mma<T>::Frag w[8 / kN];
+  __device__ inline float at(int i) const { return to_float<T>(w[i / kN][i % kN]); }
+};
+template <typename T, bool kWords>
+__device__ inline Eight<T> read_8(const T* p, int32_t many) {
+  using Word = typename Mma<T>::Frag;
+  constexpr int kN = Eight<T>::kN;
+  Eight<T> e = {};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w.v[i] = from_float<T>(v[i]);
-  *(Pack<T>*)p = w;
+  for (int i = 0; i < 8; i += kN) {
+    if (many >= i + kN) {
+      if constexpr (kWords) e.w[i / kN] = *(const Word*)(p + i);
+      else __builtin_memcpy(&e.w[i / kN], p + i, 16);
+    } else if (!kWords) {
+#pragma unroll
+      for (int x = 0; x < kN; ++x)
+        if (i + x < many) e.w[i / kN][x] = p[i + x];
+    }
+  }
+  return e;
+}
+template <typename T, bool kWords>
+__device__ inline void write_8(T* p, int32_t many, const float (&v)[8]) {
+  using Word = typename Mma<T>::Frag;
+  constexpr int kN = Eight<T>::kN;
+#pragma unroll
+  for (int i = 0; i < 8; i += kN) {
+    Word w;
+#pragma unroll
+    for (int x = 0; x < kN; ++x) w[x] = from_float<T>(v[i + x]);
+    if (kWords) {
+      if (i == 0 || many > i) *(Word*)(p + i) = w;  // (the caller has looked that there is one at all)
+    } else {
+      u32x4 word;
+      __builtin_memcpy(&word, &w, 16);
+      write_word(p + i, word, many - i);
+    }
+  }
 }
 template <int kAct, typename T>
 __device__ inline void act_8(float (&v)[8]) {
@@ -92,55 +127,55 @@ __device__ inline void slope_8(float (&v)[8], const float (&z)[8]) {
 }
 
 template <typename T>
-__device__ inline void add_8(float (&v)[8], const Pack<T>& w) {
+__device__ inline void add_8(float (&v)[8], const Eight<T>& w) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] += to_float(w.v[i]);
+  for (int i = 0; i < 8; ++i) v[i] += w.at(i);
 }
 
-// what comes after the sums: nothing, an activation of one column, swiglu's pairs
+// what comes after the sums: nothing, an activation of one column (dw: the sums of dZ as well), swiglu's pairs
 enum MoeEnd { kEndNone, kEndAct, kEndSwiglu };
 
 // Eight columns of a row of C from the sums: `bias` and `other` (forward: the residual; dx: z of the product before) have been
 // read by the caller, together for many rows.
-template <typename T, MoeOp kOp, MoeEnd kEnd>
-__device__ inline void moe_emit_8(const MoeProduct& p, int32_t act, int expert, int64_t i, int32_t j, const float* acc, const Pack<T>& bias,
-                                  const Pack<T>& other, const Pack<T>& pair) {
+template <typename T, MoeOp kOp, MoeEnd kEnd, bool kWords>
+__device__ inline void moe_emit_8(const MoeProduct& p, int32_t act, int expert, int64_t i, int32_t j, int32_t many, const float* acc,
+                                  const Eight<T>& bias, const Eight<T>& other, const Eight<T>& pair) {
   float v[8];
 #pragma unroll
   for (int x = 0; x < 8; ++x) v[x] = acc[x];
   if constexpr (kOp == kMoeForward) {
     add_8(v, bias);
-    if (p.pre) write_8((T*)p.pre + i * p.ld_pre + j, v);
+    if (p.pre) write_8<T, kWords>((T*)p.pre + i * p.ld_pre + j, many, v);
     if constexpr (kEnd == kEndAct) {
       if (act == SPTIR_ACT_RELU) act_8<SPTIR_ACT_RELU, T>(v);
       else if (act == SPTIR_ACT_GELU) act_8<SPTIR_ACT_GELU, T>(v);
       else act_8<SPTIR_ACT_SILU, T>(v);
     }
     add_8(v, other);
-    write_8((T*)p.C + i * p.ldc + j, v);
+    write_8<T, kWords>((T*)p.C + i * p.ldc + j, many, v);
   } else if constexpr (kOp == kMoeDx) {
     if constexpr (kEnd == kEndAct) {
       float z[8];
 #pragma unroll
-      for (int x = 0; x < 8; ++x) z[x] = to_float(other.v[x]);
+      for (int x = 0; x < 8; ++x) z[x] = other.at(x);
       if (act == SPTIR_ACT_RELU) slope_8<SPTIR_ACT_RELU, T>(v, z);
       else if (act == SPTIR_ACT_GELU) slope_8<SPTIR_ACT_GELU, T>(v, z);
       else slope_8<SPTIR_ACT_SILU, T>(v, z);
     } else if constexpr (kEnd == kEndSwiglu) {
       float du[8];
 #pragma unroll
-      for (int x = 0; x < 8; ++x) act_gated_slope<T>(v[x], to_float(other.v[x]), to_float(pair.v[x]), &v[x], &du[x]);
-      write_8((T*)p.C + i * p.ldc + j + p.n_j, du);
+      for (int x = 0; x < 8; ++x) act_gated_slope<T>(v[x], other.at(x), pair.at(x), &v[x], &du[x]);
+      write_8<T, kWords>((T*)p.C + i * p.ldc + j + p.n_j, many, du);
     }
-    write_8((T*)p.C + i * p.ldc + j, v);
+    write_8<T, kWords>((T*)p.C + i * p.ldc + j, many, v);
   } else {
-    write_8((T*)p.C + expert * p.c_stride + i * p.ldc + j, v);
+    write_8<T, kWords>((T*)p.C + expert * p.c_stride + i * p.ldc + j, many, v);
   }
 }
 // swiglu: eight columns of y from the sums of their gates and of what goes with them
-template <typename T>
-__device__ inline void moe_emit_gated_8(const MoeProduct& p, int64_t i, int32_t j, const float* gate, const float* up, const Pack<T>& bias_g,
-                                        const Pack<T>& bias_u, const Pack<T>& residual) {
+template <typename T, bool kWords>
+__device__ inline void moe_emit_gated_8(const MoeProduct& p, int64_t i, int32_t j, int32_t many, const float* gate, const float* up,
+                                        const Eight<T>& bias_g, const Eight<T>& bias_u, const Eight<T>& residual) {
   float g[8], u[8];
 #pragma unroll
   for (int x = 0; x < 8; ++x) { g[x] = gate[x]; u[x] = up[x]; }
@@ -148,35 +183,37 @@ __device__ inline void moe_emit_gated_8(const MoeProduct& p, int64_t i, int32_t 
   add_8(u, bias_u);
   if (p.pre) {
     T* z = (T*)p.pre + i * p.ld_pre + j;
-    write_8(z, g);
-    write_8(z + p.n_j / 2, u);
+    write_8<T, kWords>(z, many, g);
+    write_8<T, kWords>(z + p.n_j / 2, many, u);
   }
 #pragma unroll
   for (int x = 0; x < 8; ++x) g[x] = act_gated<T>(g[x], u[x]);
   add_8(g, residual);
-  write_8((T*)p.C + i * p.ldc + j, g);
+  write_8<T, kWords>((T*)p.C + i * p.ldc + j, many, g);
 }
-template <typename T, MoeOp kOp, MoeEnd kEnd>
-__device__ inline void moe_clear_8(const MoeProduct& p, int64_t i, int32_t j) {
+template <typename T, MoeOp kOp, MoeEnd kEnd, bool kWords>
+__device__ inline void moe_clear_8(const MoeProduct& p, int64_t i, int32_t j, int32_t many) {
   const float zero[8] = {};
-  write_8((T*)p.C + i * p.ldc + j, zero);
+  write_8<T, kWords>((T*)p.C + i * p.ldc + j, many, zero);
   if (kOp == kMoeForward && p.pre) {
-    write_8((T*)p.pre + i * p.ld_pre + j, zero);
-    if (kEnd == kEndSwiglu) write_8((T*)p.pre + i * p.ld_pre + j + p.n_j / 2, zero);
+    write_8<T, kWords>((T*)p.pre + i * p.ld_pre + j, many, zero);
+    if (kEnd == kEndSwiglu) write_8<T, kWords>((T*)p.pre + i * p.ld_pre + j + p.n_j / 2, many, zero);
   }
-  if (kOp == kMoeDx && kEnd == kEndSwiglu) write_8((T*)p.C + i * p.ldc + j + p.n_j, zero);
+  if (kOp == kMoeDx && kEnd == kEndSwiglu) write_8<T, kWords>((T*)p.C + i * p.ldc + j + p.n_j, many, zero);
 }
 
 // the tiles' kernels count 16-byte words of an operand with 32 bits
-inline bool moe_near(int64_t rows, int64_t ld) { return rows == 0 || ld < ((int64_t)1 << 34) / rows; }
+inline bool moe_near(int32_t type, int64_t rows, int64_t ld) {
+  return rows == 0 || ld < ((int64_t)1 << 32) * (16 / moe_type_bytes(type)) / rows;
+}
 
-// ---- launches (moe_few.hip: any alignment; moe_tiles.hip: 16-byte words)
+// ---- launches (moe_few.hip, moe_tiles.hip; words: in 16-byte words throughout)
 double moe_few_estimate(int32_t type, const MoeProduct& p, int32_t* fragments);  // microseconds
 sptir_status_t moe_few_forward(int32_t type, int32_t act, const MoeProduct& p, int32_t fragments, hipStream_t stream);
-double moe_tiles_forward_estimate(int32_t act, const MoeProduct& p);
-sptir_status_t moe_tiles_forward(int32_t type, int32_t act, const MoeProduct& p, hipStream_t stream);
-sptir_status_t moe_tiles_dx(int32_t type, int32_t act, const MoeProduct& p, hipStream_t stream);
-sptir_status_t moe_tiles_dw(int32_t type, const MoeProduct& p, hipStream_t stream);
+double moe_tiles_forward_estimate(int32_t type, int32_t act, bool words, const MoeProduct& p);
+sptir_status_t moe_tiles_forward(int32_t type, int32_t act, bool words, const MoeProduct& p, hipStream_t stream);
+sptir_status_t moe_tiles_dx(int32_t type, int32_t act, bool words, const MoeProduct& p, hipStream_t stream);
+sptir_status_t moe_tiles_dw(int32_t type, bool words, const MoeProduct& p, hipStream_t stream);
 
 }  // namespace sptir
 

@@ -1,5 +1,4 @@
-// The experts' products of float16 and bfloat16 in large tiles: operands from memory straight to LDS, matrix instructions
-// from there.
+// The experts' products in large tiles: operands from memory to LDS, matrix instructions from there.
 #include <algorithm>
 #include <cmath>
 #include <utility>
@@ -19,29 +18,27 @@ __device__ inline void to_lds(const void* from, lds_char* to) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
-// kBR: of r, a step; kStages: steps that LDS holds
-template <int kBM_, int kBN_, int kWavesM_, int kWavesN_, int kBR_, int kStages_, int kGroups_>
+// A step takes 128 bytes of r: 64 elements of 16 bits, 32 of float32.  kStages: steps that LDS holds.
+template <int kBM_, int kBN_, int kWavesM_, int kWavesN_, int kStages_, int kGroups_>
 struct Shape {
-  static constexpr int kBM = kBM_, kBN = kBN_, kWavesM = kWavesM_, kWavesN = kWavesN_, kBR = kBR_, kStages = kStages_;
+  static constexpr int kBM = kBM_, kBN = kBN_, kWavesM = kWavesM_, kWavesN = kWavesN_, kStages = kStages_;
   static constexpr int kGroups = kGroups_;  // workgroups that a CU holds
   static constexpr int kThreads = 64 * kWavesM * kWavesN, kWavesPerSimd = kGroups * kThreads / 256;
   static constexpr int kFM = kBM / kWavesM / 16, kFN = kBN / kWavesN / 16;  // fragments of a wavefront's tile
   static_assert(kFN == 4, "a wavefront has 64 columns");
-  static constexpr int kBytesA = kBM * kBR * 2, kBytesB = kBN * kBR * 2, kStage = kBytesA + kBytesB;
+  static constexpr int kBytesA = kBM * 128, kBytesB = kBN * 128, kStage = kBytesA + kBytesB;
   static constexpr int kLds = kStages * kStage + (int)sizeof(MoeTable);
   static_assert(kGroups * kLds <= 160 * 1024, "LDS");
 };
 
 // Which 16-byte chunk of a line lies at place `pos` of it in LDS: pos ^ key(line), so that the lanes that read together find
 // their chunks in different banks.  (Lines along r: of a step's r; lines across: of the tile's rows or columns.)
-template <int kChunks>
-__device__ inline int key_rows(int row) { return kChunks == 8 ? row & 7 : (row >> 1) & 3; }
+__device__ inline int key_rows(int row) { return row & 7; }
 // the columns are read four from every 16: rows 16 w + 4 g + v of LDS by lanes 4 w + v
-template <int kChunks>
-__device__ inline int key_cols(int row) { return kChunks == 8 ? (row & 3) | ((row >> 4) & 1) << 2 : ((row >> 1) & 1) | ((row >> 4) & 1) << 1; }
+__device__ inline int key_cols(int row) { return (row & 3) | ((row >> 4) & 1) << 2; }
 // lines across, read by the transposing instruction: four lines at once, 16 rows of them in two chunks ...
 __device__ inline int key_tr_rows(int r) { return (r & 3) << 1 | ((r >> 3) & 1) << 3; }
-// ... or four columns from every 16 of 64
+// ... or four columns from every 16 of 64.  (float32: 16 chunks next to each other are read, and lie as they are.)
 __device__ inline int key_tr_cols(int r) { return (r & 1) | ((r >> 1) & 1) << 3; }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -62,6 +59,8 @@ __device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>)
 template <int N, typename F>
 __device__ __forceinline__ void each(F&& f) { each_of(f, std::make_integer_sequence<int, N>{}); }
 
+constexpr int kNoWait = 63;  // (the counter's most: nothing to wait for)
+
 // All but this wavefront's last kLeft memory operations are done, and its reads of LDS; then all wavefronts'.  (Nothing is
 // moved across.)
 template <int kLeft>
@@ -71,22 +70,32 @@ __device__ inline void arrive_and_meet() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-template <typename T, MoeOp kOp, MoeEnd kEnd, typename S>
+// All of this wavefront's memory operations are done.  (Said where something is read that need not be: behind the place where
+// the ways meet again the compiler would wait on both of them, for the stores before it too.)
+__device__ inline void loads_arrived() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+
+// kWords: the operands, and what the epilogue reads and writes, lie in 16-byte words: chunks go from memory to LDS by
+// themselves, and their places are counted in words with 32 bits.  Otherwise a thread reads them from where they are and
+// writes them to LDS a step later.
+template <typename T, MoeOp kOp, MoeEnd kEnd, bool kWords, typename S>
 __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(MoeProduct p, int32_t act, int32_t j_tiles, int32_t i_tiles) {
   extern __shared__ __attribute__((aligned(16))) char lds_generic[];
   lds_char* lds = (lds_char*)lds_generic;
-  constexpr int kThreads = S::kThreads, kBR = S::kBR;
+  constexpr bool k16 = sizeof(T) == 2;
+  constexpr int kN = 16 / sizeof(T), kThreads = S::kThreads, kBR = 8 * kN;  // elements of a chunk; of r, a step
   constexpr bool kAAlongR = kOp != kMoeDw, kBAlongR = kOp == kMoeForward;
   constexpr bool kGated = kOp == kMoeForward && kEnd == kEndSwiglu;  // (C has half the columns)
   constexpr int kColsC = kGated ? S::kBN / 2 : S::kBN;
+  static_assert(k16 || kAAlongR || S::kFM == 4, "rows of float32 lines across are taken by four");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t out_cols = kGated ? p.n_j / 2 : p.n_j;
 
-  constexpr int kLineA = kAAlongR ? kBR / 8 : S::kBM / 8, kLineB = kBAlongR ? kBR / 8 : S::kBN / 8;  // chunks of a line
-  constexpr int kLoadsA = S::kBytesA / 16 / kThreads, kLoadsB = S::kBytesB / 16 / kThreads;
+  constexpr int kLineA = kAAlongR ? 8 : S::kBM / kN, kLineB = kBAlongR ? 8 : S::kBN / kN;  // chunks of a line
+  constexpr int kLoadsA = S::kBytesA / 16 / kThreads, kLoadsB = S::kBytesB / 16 / kThreads, kLoads = kLoadsA + kLoadsB;
   constexpr int kStepA = kThreads / kLineA, kStepB = kThreads / kLineB;  // lines between a thread's loads
   const int line_a = tid / kLineA, line_b = tid / kLineB;
-  const int wi = wave / S::kWavesN * (S::kFM * 16), wj = wave % S::kWavesN * (S::kFN * 16), fr = lane & 15, q = lane >> 4;
+  const int wm = wave / S::kWavesN, wn = wave % S::kWavesN;
+  const int wi = wm * (S::kFM * 16), wj = wn * (S::kFN * 16), fr = lane & 15, q = lane >> 4;
 
   // ---- the tiles of this workgroup
   const uint32_t per_expert = (uint32_t)i_tiles * j_tiles;
@@ -97,13 +106,31 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   int32_t j0;
   int64_t r0 = 0, r1 = p.n_r;
   int steps = 0;
-  // the places of this thread's chunks in their operands, in units of 16 bytes, from the step's base on
-  uint32_t a_at[kLoadsA], b_at[kLoadsB];
-  const char *a_base, *b_base;
 
-  // What this thread brings to LDS of a tile.  Rows and columns past the tile's end take the last there is (nothing of them
-  // is written); r past its end takes zeros, in both operands, whatever lies there.
-  auto start = [&](uint32_t id) {
+  // What a thread brings to LDS of a tile: chunk_a(n) and chunk_b(n) of the line a_line(n), b_line(n) of every step.  Rows and
+  // columns past the tile's end take the last there is, or zeros (nothing of them is written); r past its end takes zeros, in
+  // both operands, whatever lies there.
+  auto a_line = [&](int n) { return line_a + n * kStepA; };
+  auto b_line = [&](int n) { return line_b + n * kStepB; };
+  auto chunk_a = [&](int n) { return tid % kLineA ^ (kAAlongR ? key_rows(a_line(n)) : k16 ? key_tr_rows(a_line(n)) : 0); };
+  auto chunk_b = [&](int n) { return tid % kLineB ^ (kBAlongR ? key_cols(b_line(n)) : k16 ? key_tr_cols(b_line(n)) : 0); };
+  auto a_row = [&](int n) { return min(t.first + a_line(n), t.end - 1); };  // lines along r: the sorted row
+  auto b_row = [&](int n) {  // (forward) the row of W[e]; gated: of 16 lines 8 gates, then the 8 that go with them
+    const int line = b_line(n);
+    if (kGated) return min(j0 + line / 16 * 8 + line % 8, out_cols - 1) + (line & 8 ? out_cols : 0);
+    return min(j0 + line, p.n_j - 1);
+  };
+  // kWords: places in units of 16 bytes from the step's base on.  Otherwise addresses, and what was read for a later step.
+  constexpr int kPlaces = kWords ? kLoads : 1, kHeld = kWords ? 1 : kLoads;
+  uint32_t place[kPlaces];
+  const char *a_base, *b_base;
+  const T* from[kHeld];
+  u32x4 held[kHeld];
+  const int64_t a_step = (kAAlongR ? kBR : kBR * p.lda) * (int64_t)sizeof(T), b_step = (kBAlongR ? kBR : kBR * p.ldb) * (int64_t)sizeof(T);
+
+  constexpr bool kSumZ = kOp == kMoeDw && kEnd != kEndNone;  // (db is asked for)
+  bool sum_z = false;  // this tile's workgroup sums dZ too
+  auto start = [&](uint32_t id) __attribute__((always_inline)) {
     const uint32_t dealt = moe_deal(id, total);
     int jt;
     if constexpr (kOp == kMoeDw) {
@@ -113,6 +140,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
       t = {e, (int64_t)it * S::kBM, p.n_i};
       r0 = p.expert_ptr ? p.expert_ptr[e] : 0;
       r1 = p.expert_ptr ? p.expert_ptr[e + 1] : p.n_rows;
+      sum_z = kSumZ && jt == 0;
     } else {
       int mt;
       moe_square(dealt, m_tiles, j_tiles, &mt, &jt);
@@ -122,117 +150,176 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
     const bool none = kOp != kMoeDw && t.expert == p.n_experts;
     steps = r1 > r0 && !none ? (int)((r1 - r0 + kBR - 1) / kBR) : 0;
     if (none) return;
-    a_base = (const char*)p.A + (kAAlongR ? 0 : r0 * p.lda * 2);
-    b_base = (const char*)p.B + (kOp == kMoeDw ? 0 : t.expert * p.b_stride * 2);
-    each<kLoadsA>([&](auto nth) {
-      constexpr int n = decltype(nth)::value;
-      const int line = line_a + n * kStepA;
-      if constexpr (kAAlongR) {
-        const int64_t s = min(t.first + line, t.end - 1);
-        a_at[n] = (uint32_t)(((kOp == kMoeForward ? moe_x_row(p, s) : s) * p.lda >> 3) + (tid % kLineA ^ key_rows<kLineA>(line)));
+    const int64_t b_expert = kOp == kMoeDw ? 0 : t.expert * p.b_stride;
+    a_base = (const char*)p.A + (kAAlongR ? 0 : r0 * p.lda * (int64_t)sizeof(T));
+    b_base = (const char*)p.B + b_expert * (int64_t)sizeof(T);
+    int64_t rows[kAAlongR ? kLoadsA : 1];
+    if constexpr (kAAlongR) {
+      each<kLoadsA>([&](auto n) { rows[n] = a_row(n); });
+      if (kOp == kMoeForward && p.entry_of) {  // (all of them asked for before the first is waited for)
+        int32_t entry[kLoadsA];
+        each<kLoadsA>([&](auto n) { entry[n] = p.entry_of[rows[n]]; });
+        each<kLoadsA>([&](auto n) { rows[n] = moe_token(p, entry[n]); });
+      }
+    }
+    each<kLoadsA>([&](auto n) {
+      const int c = chunk_a(n);
+      if constexpr (kWords) {
+        if constexpr (kAAlongR) place[n] = (uint32_t)(rows[n] * p.lda / kN + c);
+        else place[n] = (uint32_t)((a_line(n) * p.lda + min(t.first + c * kN, t.end - kN)) / kN);
       } else {
-        const int64_t col = t.first + (tid % kLineA ^ key_tr_rows(line)) * 8;
-        a_at[n] = (uint32_t)((line * p.lda + min(col, t.end - 8)) >> 3);
+        if constexpr (kAAlongR) from[n] = (const T*)p.A + rows[n] * p.lda + c * kN;
+        else from[n] = (const T*)p.A + (r0 + a_line(n)) * p.lda + t.first + c * kN;
       }
     });
     each<kLoadsB>([&](auto nth) {
-      constexpr int n = decltype(nth)::value;
-      const int line = line_b + n * kStepB;
-      if constexpr (kBAlongR) {
-        int32_t w;
-        if (kGated) {  // of 16 lines: 8 gates, then the 8 that go with them
-          w = min(j0 + line / 16 * 8 + line % 8, out_cols - 1) + (line & 8 ? out_cols : 0);
-        } else {
-          w = min(j0 + line, p.n_j - 1);
-        }
-        b_at[n] = (uint32_t)((w * p.ldb >> 3) + (tid % kLineB ^ key_cols<kLineB>(line)));
+      constexpr int n = decltype(nth)::value, m = kLoadsA + n;
+      const int c = chunk_b(n);
+      if constexpr (kWords) {
+        if constexpr (kBAlongR) place[m] = (uint32_t)(b_row(n) * p.ldb / kN + c);
+        else place[m] = (uint32_t)(((kOp == kMoeDx ? b_line(n) * p.ldb : 0) + min(j0 + c * kN, p.n_j - kN)) / kN);
       } else {
-        const int32_t col = min(j0 + (tid % kLineB ^ key_tr_cols(line)) * 8, p.n_j - 8);
-        b_at[n] = (uint32_t)((kOp == kMoeDx ? line * p.ldb + col : col) >> 3);
+        if constexpr (kBAlongR) from[m] = (const T*)p.B + b_expert + b_row(n) * p.ldb + c * kN;
+        else from[m] = (const T*)p.B + b_expert + (kOp == kMoeDx ? b_line(n) * p.ldb : 0) + j0 + c * kN;
       }
     });
   };
-  const int64_t a_step = (kAAlongR ? kBR : kBR * p.lda) * 2, b_step = (kBAlongR ? kBR : kBR * p.ldb) * 2;
-  // the n-th of a thread's loads of a step; `whole`: r does not end in it
-  constexpr int kLoads = kLoadsA + kLoadsB;
-  auto load_one = [&](int step, int into, auto nth, auto all) {
+  // (dw) The entries whose tokens' rows of X a step loads, asked for a step earlier: to wait for one that has just been asked
+  // for would be to wait for all loads before it.
+  int32_t entry[kOp == kMoeDw ? kLoadsB : 1] = {};
+  auto ask = [&](int step) __attribute__((always_inline)) {
+    if constexpr (kOp == kMoeDw) {
+      if (!p.entry_of || step >= steps) return;
+      each<kLoadsB>([&](auto n) { entry[n] = p.entry_of[min(r0 + (int64_t)step * kBR + b_line(n), r1 - 1)]; });
+    }
+  };
+  auto x_row = [&](int step, int n) { return p.entry_of ? moe_token(p, entry[n]) : r0 + (int64_t)step * kBR + b_line(n); };
+  // (without kWords) the length of the n-th chunk's line, and how far the chunk's end is past its end
+  auto line_length = [&](int n) { return n < kLoadsA ? (kAAlongR ? p.n_r : p.n_i) : (kBAlongR ? p.n_r : p.n_j); };
+  auto past_end = [&](int step, int n) {
+    const bool kA = n < kLoadsA;
+    const int chunk = kA ? chunk_a(n) : chunk_b(n - kLoadsA);
+    const int64_t at = (kA ? kAAlongR : kBAlongR) ? (int64_t)step * kBR : kA ? t.first : (int64_t)j0;
+    return (int)(at + (chunk + 1) * kN - line_length(n));
+  };
+  // The n-th of a thread's loads of a step; `whole`: r does not end in it.
+  auto load_one = [&](int step, int into, auto nth, auto all) __attribute__((always_inline)) {
     constexpr int n = decltype(nth)::value;
-    constexpr bool whole = decltype(all)::value;
-    lds_char* to = lds + into * S::kStage + (n * kThreads + wave * 64) * 16;
+    constexpr bool whole = decltype(all)::value, kA = n < kLoadsA, kAlong = kA ? kAAlongR : kBAlongR;
+    constexpr int m = kA ? n : n - kLoadsA;
     const int64_t left = r1 - r0 - (int64_t)step * kBR;
-    const char* from;
-    int r;
-    if constexpr (n < kLoadsA) {
-      const int line = line_a + n * kStepA;
-      r = kAAlongR ? (tid % kLineA ^ key_rows<kLineA>(line)) * 8 : line;
-      from = a_base + (uint64_t)a_at[n] * 16;
+    const int line = kA ? a_line(m) : b_line(m), chunk = kA ? chunk_a(m) : chunk_b(m);
+    const int r = kAlong ? chunk * kN : line;
+    if constexpr (kWords) {
+      const char* at = (kA ? a_base : b_base) + (uint64_t)place[n] * 16;
+      if constexpr (!kA && kOp == kMoeDw) at += x_row(step, m) * p.ldb * (int64_t)sizeof(T);
+      if (!whole && r >= left) at = (const char*)g_zero;
+      to_lds(at, lds + into * S::kStage + (n * kThreads + wave * 64) * 16);
     } else {
-      constexpr int m = n - kLoadsA;
-      const int line = line_b + m * kStepB;
-      r = kBAlongR ? (tid % kLineB ^ key_cols<kLineB>(line)) * 8 : line;
-      from = b_base + (uint64_t)b_at[m] * 16;
-      if (kOp == kMoeDw && (whole || r < left)) from += moe_x_row(p, r0 + (int64_t)step * kBR + r) * p.ldb * 2;
+      // (the line's last 16 bytes where it ends before the chunk does: put() moves them to their place)
+      const T* at = from[n];
+      if constexpr (!kA && kOp == kMoeDw) at += x_row(step, m) * p.ldb;
+      const bool there = kAlong || whole || r < left;
+      const int over = past_end(step, n);
+      if (line_length(n) >= kN) {
+        at = there ? at - max(over, 0) : kA ? (const T*)p.A : (const T*)p.B;
+        __builtin_memcpy(&held[n], at, 16);
+      } else {
+        held[n] = read_elements(at, there ? min(kN - over, kN) : 0);
+      }
+      if (kA || kOp != kMoeDw) from[n] = (const T*)((const char*)from[n] + (kA ? a_step : b_step));
     }
-    if (!whole && r >= left) from = (const char*)g_zero;
-    to_lds(from, to);
   };
-  auto next_step = [&] {
-    a_base += a_step;
-    if (kOp != kMoeDw) b_base += b_step;
-  };
-  auto load = [&](int step, int into) {
-    const bool whole = (int64_t)(step + 1) * kBR <= r1 - r0;
-    if (whole) {
-      each<kLoads>([&](auto n) { load_one(step, into, n, std::true_type{}); });
-    } else {
-      each<kLoads>([&](auto n) { load_one(step, into, n, std::false_type{}); });
+  auto load = [&](int step, int into) __attribute__((always_inline)) {
+    const bool whole = kWords && (int64_t)(step + 1) * kBR <= r1 - r0;
+    if (whole) each<kLoads>([&](auto n) { load_one(step, into, n, std::true_type{}); });
+    else each<kLoads>([&](auto n) { load_one(step, into, n, std::false_type{}); });
+    if constexpr (kWords) {
+      a_base += a_step;
+      if (kOp != kMoeDw) b_base += b_step;
     }
-    next_step();
+    ask(step + 1);
+  };
+  auto put = [&](int step, int into) __attribute__((always_inline)) {  // (without kWords) what is held, into LDS
+    const bool whole = (int64_t)(step + 1) * kBR <= r1 - r0 && ((kAAlongR || t.first + S::kBM <= t.end) && (kBAlongR || j0 + S::kBN <= p.n_j));
+    each<kHeld>([&](auto nth) {
+      constexpr int n = decltype(nth)::value;
+      constexpr bool kA = n < kLoadsA, kAlong = kA ? kAAlongR : kBAlongR;
+      if (!whole) {
+        const bool there = kAlong || (kA ? a_line(n) : b_line(n - kLoadsA)) < r1 - r0 - (int64_t)step * kBR;
+        const int over = past_end(step, n);
+        if (line_length(n) >= kN) held[n] = without_first(held[n], there ? max(over, 0) * (int)sizeof(T) : 16);
+      }
+      *(__attribute__((address_space(3))) u32x4*)(lds + into * S::kStage + (n * kThreads + tid) * 16) = held[n];
+    });
   };
 
   // ---- products
   using M = Mma<T>;
   using Frag = typename M::Frag;
-  auto read_a = [&](lds_char* stage, int kk, int f) -> Frag {
-    if constexpr (kAAlongR) {
-      const int row = wi + 16 * f + fr;
-      return *(__attribute__((address_space(3))) Frag*)(stage + row * (kLineA * 16) + ((kk * 4 + q) ^ key_rows<kLineA>(fr)) * 16);
-    } else {
-      const int r = kk * 32 + q * 8 + (fr >> 2), col = wi + 16 * f + (fr & 3) * 4;
-      const int r4 = (fr >> 2) | (q & 1) << 3;  // (what of r the key looks at)
-      lds_char* at = stage + r * (kLineA * 16) + ((col >> 3) ^ key_tr_rows(r4)) * 16 + (col & 4) * 2;
-      return read_tr<Frag>(at, 4 * kLineA * 16);
-    }
-  };
-  auto read_b = [&](lds_char* stage, int kk, int g) -> Frag {
-    stage += S::kBytesA;
-    if constexpr (kBAlongR) {
-      const int row = wj + (fr >> 2) * 16 + g * 4 + (fr & 3);
-      return *(__attribute__((address_space(3))) Frag*)(stage + row * (kLineB * 16) + ((kk * 4 + q) ^ key_cols<kLineB>((fr & 3) | (fr & 4) << 2)) * 16);
-    } else {
-      const int r = kk * 32 + q * 8 + (fr >> 2), col = wj + (fr & 3) * 16 + g * 4;
-      lds_char* at = stage + r * (kLineB * 16) + ((col >> 3) ^ key_tr_cols(fr >> 2)) * 16 + (col & 4) * 2;
-      return read_tr<Frag>(at, 4 * kLineB * 16);
-    }
-  };
-  f32x4 acc[S::kFM][S::kFN];
-  // A phase multiplies two fragments of rows with the columns', 32 of r, while the fragments of the next phase are read.
-  constexpr int kPhases = S::kFM / 2, kParts = kBR / 32;
+  f32x4 acc[S::kFM][S::kFN], acc_z[2];
+  // A phase multiplies two fragments of rows with the columns', 64 bytes of r, while the fragments of the next phase are read.
+  constexpr int kPhases = S::kFM / 2, kParts = 2;
   static_assert(kPhases % 2 == 0, "the sets of fragments alternate");
   Frag a[2][2], b[2][S::kFN];
-  auto read_rows = [&](int stage, int kk, auto phase) {
+  auto read_rows = [&](int stage, int kk, auto phase) __attribute__((always_inline)) {
     constexpr int ph = decltype(phase)::value;
-    each<2>([&](auto f) { a[ph & 1][f] = read_a(lds + stage * S::kStage, kk, ph * 2 + f); });
+    lds_char* base = lds + stage * S::kStage;
+    if constexpr (kAAlongR) {
+      each<2>([&](auto f) {
+        a[ph & 1][f] = *(__attribute__((address_space(3))) Frag*)(base + (wi + 16 * (ph * 2 + f) + fr) * 128 + ((kk * 4 + q) ^ key_rows(fr)) * 16);
+      });
+    } else if constexpr (k16) {
+      each<2>([&](auto f) {
+        const int r = kk * 32 + q * 8 + (fr >> 2), row = wi + 16 * (ph * 2 + f) + (fr & 3) * 4;
+        const int r4 = (fr >> 2) | (q & 1) << 3;  // (what of r the key looks at)
+        a[ph & 1][f] = read_tr<Frag>(base + r * (kLineA * 16) + ((row >> 3) ^ key_tr_rows(r4)) * 16 + (row & 4) * 2, 4 * kLineA * 16);
+      });
+    } else {  // lane: rows 4 fr + 2 ph and the next, of four lines
+      typedef float f32x2 __attribute__((ext_vector_type(2)));
+      each<4>([&](auto x) {
+        const f32x2 two = *(__attribute__((address_space(3))) f32x2*)(base + (kk * 16 + q * 4 + x) * (kLineA * 16) + (wi + fr * 4 + ph * 2) * 4);
+        constexpr int e = decltype(x)::value;
+        a[ph & 1][0][e] = two[0];
+        a[ph & 1][1][e] = two[1];
+      });
+    }
   };
-  auto read_cols = [&](int stage, int kk, auto set) {
-    each<S::kFN>([&](auto g) { b[decltype(set)::value][g] = read_b(lds + stage * S::kStage, kk, g); });
+  auto read_cols = [&](int stage, int kk, auto which) __attribute__((always_inline)) {
+    constexpr int set = decltype(which)::value;
+    lds_char* base = lds + stage * S::kStage + S::kBytesA;
+    if constexpr (kBAlongR) {
+      each<4>([&](auto g) {
+        const int row = wj + (fr >> 2) * 16 + g * 4 + (fr & 3);
+        b[set][g] = *(__attribute__((address_space(3))) Frag*)(base + row * 128 + ((kk * 4 + q) ^ key_cols((fr & 3) | (fr & 4) << 2)) * 16);
+      });
+    } else if constexpr (k16) {
+      each<4>([&](auto g) {
+        const int r = kk * 32 + q * 8 + (fr >> 2), col = wj + (fr & 3) * 16 + g * 4;
+        b[set][g] = read_tr<Frag>(base + r * (kLineB * 16) + ((col >> 3) ^ key_tr_cols(fr >> 2)) * 16 + (col & 4) * 2, 4 * kLineB * 16);
+      });
+    } else {  // lane: columns 4 fr .. 4 fr + 3 of four lines
+      each<4>([&](auto x) {
+        const f32x4 four = *(__attribute__((address_space(3))) f32x4*)(base + (kk * 16 + q * 4 + x) * (kLineB * 16) + (wj + fr * 4) * 4);
+        each<4>([&](auto g) { b[set][g][decltype(x)::value] = four[decltype(g)::value]; });
+      });
+    }
   };
-  auto multiply = [&](auto set, auto phase) {
-    constexpr int ph = decltype(phase)::value;
+  auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+  auto multiply = [&](auto set, auto phase) __attribute__((always_inline)) {
+    constexpr int ph = decltype(phase)::value, kSet = decltype(set)::value;
     each<2>([&](auto f) {
-      each<S::kFN>([&](auto g) { acc[ph * 2 + f][g] = M::run(b[decltype(set)::value][g], a[ph & 1][f], acc[ph * 2 + f][g]); });
+      each<4>([&](auto g) { acc[ph * 2 + f][g] = M::run(b[kSet][g], a[ph & 1][f], acc[ph * 2 + f][g]); });
     });
+    if constexpr (kSumZ) {  // dZ times ones: the wavefronts that share rows take a phase's each
+      if (sum_z && wn == ph) {
+        Frag ones;
+        each<kN>([&](auto x) { ones[decltype(x)::value] = from_float<T>(1.f); });
+        each<2>([&](auto f) { acc_z[f] = M::run(ones, a[ph & 1][f], acc_z[f]); });
+      }
+    }
   };
+  static_assert(kOp != kMoeDw || S::kWavesN == kPhases, "a wavefront for every phase");
 
   // One step.  The barrier before its last phase says that this step's part of LDS has been read and that the next step's is
   // there; the loads of kStages - 2 more steps may still be on their way.  The order of a phase is kept as it is written
@@ -243,14 +330,12 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   constexpr int kStores = S::kFM * (kGated ? 1 : 2);
   bool stored = false;
   int stage = 0;
-  auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
-  auto run_step = [&](int s, auto first_set) {
-    constexpr int kFirst = decltype(first_set)::value;
+  auto run_step = [&](int s) __attribute__((always_inline)) {
     const int next = S::kStages == 2 ? stage ^ 1 : stage + 1 == S::kStages ? 0 : stage + 1;
     each<kParts>([&](auto part) {
-      constexpr int kk = decltype(part)::value, kSet = (kFirst + kk) & 1;
-      constexpr std::integral_constant<int, kSet> set{};
-      constexpr std::integral_constant<int, kSet ^ 1> other{};
+      constexpr int kk = decltype(part)::value;
+      constexpr std::integral_constant<int, kk> set{};
+      constexpr std::integral_constant<int, kk ^ 1> other{};
       each<kPhases - 1>([&](auto phase) {
         read_rows(stage, kk, std::integral_constant<int, decltype(phase)::value + 1>{});
         fence();
@@ -265,27 +350,35 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
         multiply(set, last);
         fence();
       } else {
-        if (S::kStages > 2 && s + S::kStages <= steps) arrive_and_meet<(S::kStages - 2) * kLoads>();
+        if (!kWords) arrive_and_meet<kNoWait>();
+        else if (S::kStages > 2 && s + S::kStages <= steps) arrive_and_meet<(S::kStages - 2) * kLoads>();
         else arrive_and_meet<0>();
         if (s + 1 < steps) {
           read_cols(next, 0, other);
           read_rows(next, 0, Set0{});
         }
         fence();
-        if (s + S::kStages < steps) load(s + S::kStages, stage);
+        if constexpr (kWords) {
+          if (s + S::kStages < steps) load(s + S::kStages, stage);
+        } else {
+          if (s + S::kStages < steps) put(s + S::kStages, stage);
+          if (s + S::kStages + 1 < steps) load(s + S::kStages + 1, 0);
+        }
         multiply(set, last);
         fence();
       }
     });
     stage = next;
   };
-  using Set1 = std::integral_constant<int, kParts & 1>;  // (of the step after one that began with set 0)
 
-  auto load_first = [&] {
+  auto load_first = [&]() __attribute__((always_inline)) {
     stage = 0;
-#pragma unroll
-    for (int s = 0; s < S::kStages; ++s)
-      if (s < steps) load(s, s);
+    ask(0);
+    if constexpr (kWords) {
+      each<S::kStages>([&](auto s) { if (s < steps) load(s, s); });
+    } else {
+      if (steps > 0) load(0, 0);
+    }
   };
   uint32_t id = blockIdx.x;
   if (id >= total) return;
@@ -293,85 +386,108 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   load_first();
   while (true) {
     each<S::kFM>([&](auto f) { each<S::kFN>([&](auto g) { acc[f][g] = f32x4{0.f, 0.f, 0.f, 0.f}; }); });
+    if (kSumZ) each<2>([&](auto f) { acc_z[f] = f32x4{0.f, 0.f, 0.f, 0.f}; });
     if (steps > 0) {
-      if (stored && steps >= S::kStages) arrive_and_meet<(S::kStages - 1) * kLoads + kStores>();
-      else if (steps >= S::kStages) arrive_and_meet<(S::kStages - 1) * kLoads>();
-      else arrive_and_meet<0>();
+      if constexpr (!kWords) {
+#pragma unroll 1
+        for (int s = 0; s < S::kStages && s < steps; ++s) {
+          put(s, s);
+          if (s + 1 < steps) load(s + 1, 0);
+        }
+        arrive_and_meet<kNoWait>();
+      } else if (stored && steps >= S::kStages) {
+        arrive_and_meet<(S::kStages - 1) * kLoads + kStores>();
+      } else if (steps >= S::kStages) {
+        arrive_and_meet<(S::kStages - 1) * kLoads>();
+      } else {
+        arrive_and_meet<0>();
+      }
       read_cols(0, 0, Set0{});
       read_rows(0, 0, Set0{});
     }
-    if constexpr (kParts % 2 == 0) {
-      for (int s = 0; s < steps; ++s) run_step(s, Set0{});
-    } else {
-      int s = 0;
-      for (; s + 1 < steps; s += 2) {
-        run_step(s, Set0{});
-        run_step(s + 1, Set1{});
-      }
-      if (s < steps) run_step(s, Set0{});
-    }
+    for (int s = 0; s < steps; ++s) run_step(s);
     // the next tile's first loads run beside this one's epilogue
     const MoeTile done = t;
     const int32_t done_j0 = j0;
+    const bool done_sum_z = sum_z;
     id += gridDim.x;
     const bool more = id < total;
     if (more) {
       start(id);
       load_first();
     }
-    // a lane has row 16 f + lane % 16 and, of the wavefront's 64 columns, the 16 from (lane / 16) * 16 on (gated: 8, and
-    // their pairs).  What is read beside the sums is read for two rows at once, before their stores: loads and
-    // stores are waited for in order.
+    // A lane has the row 16 f + lane % 16 (float32 lines across: 4 (lane % 16) + f) and, of the wavefront's 64 columns, the 16
+    // from (lane / 16) * 16 on (gated: 8, and their pairs).  What is read beside the sums is read for a row or two at once, before
+    // their stores: loads and stores are waited for in order.
     // (From here on the lane's place is computed anew, or the compiler would hold what it is worth through the loop above.)
     int my_lane = lane;
     asm volatile("" : "+v"(my_lane));
-    const int my_row = wi + (my_lane & 15), my_q = my_lane >> 4;
+    constexpr int kRowApart = k16 || kAAlongR ? 16 : 1;
+    const int my_row = wi + (my_lane & 15) * (k16 || kAAlongR ? 1 : 4), my_q = my_lane >> 4;
     const bool none = kOp != kMoeDw && done.expert == p.n_experts;
     const int32_t my_j = done_j0 + (kGated ? wj / 2 + my_q * 8 : wj + my_q * 16);
+    const T* other_at = (const T*)(kOp == kMoeForward ? p.residual : p.pre);
+    const int64_t other_ld = kOp == kMoeForward ? p.ld_residual : p.ld_pre;
     if (none) {
-      each<S::kFM>([&](auto f) {
-        const int64_t i = done.first + my_row + 16 * f;
+      for (int f = 0; f < S::kFM; ++f) {
+        const int64_t i = done.first + my_row + kRowApart * f;
         each<kGated ? 1 : 2>([&](auto x) {
-          if (i < done.end && my_j + x * 8 < out_cols) moe_clear_8<T, kOp, kEnd>(p, i, my_j + x * 8);
+          const int32_t j = my_j + x * 8;
+          if (i < done.end && j < out_cols) moe_clear_8<T, kOp, kEnd, kWords>(p, i, j, out_cols - j);
         });
-      });
+      }
     } else {
       const bool other_too = kOp == kMoeForward ? p.residual != nullptr : kOp == kMoeDx && kEnd != kEndNone;
-      const T* other_at = (const T*)(kOp == kMoeForward ? p.residual : p.pre);
-      const int64_t other_ld = kOp == kMoeForward ? p.ld_residual : p.ld_pre;
-      Pack<T> bias[2] = {}, other[2][2] = {}, pair[2][2] = {};  // (what there is none of adds zeros)
-      each<S::kFM / 2>([&](auto fs) {
+      Eight<T> bias[2] = {}, other[2][2] = {}, pair[2][2] = {};  // (what there is none of adds zeros)
+      constexpr int kAtOnce = kOp == kMoeDx && kEnd == kEndSwiglu ? 1 : 2;  // (what is read is twice as much there)
+      each<S::kFM / kAtOnce>([&](auto fs) {
         if (kOp == kMoeForward && p.bias) {
-          const T* at = (const T*)p.bias + done.expert * p.bias_stride;
-          each<2>([&](auto x) { bias[x] = *(const Pack<T>*)(at + (kGated ? min(my_j, out_cols - 8) + x * out_cols : min(my_j + x * 8, out_cols - 8))); });
+          const T* at = (const T*)p.bias + done.expert * p.bias_stride + my_j;
+          each<2>([&](auto x) { bias[x] = read_8<T, kWords>(at + (kGated ? x * out_cols : x * 8), out_cols - my_j - (kGated ? 0 : x * 8)); });
+          loads_arrived();
         }
         if (other_too) {
-          each<2>([&](auto f) {
-            const T* at = other_at + min(done.first + my_row + 16 * (fs * 2 + f), done.end - 1) * other_ld;
+          each<kAtOnce>([&](auto f) {
+            const T* at = other_at + min(done.first + my_row + kRowApart * (fs * kAtOnce + f), done.end - 1) * other_ld + my_j;
             each<kGated ? 1 : 2>([&](auto x) {
-              const int32_t j = min(my_j + x * 8, out_cols - 8);
-              other[f][x] = *(const Pack<T>*)(at + j);
-              if constexpr (kOp == kMoeDx && kEnd == kEndSwiglu) pair[f][x] = *(const Pack<T>*)(at + j + p.n_j);
+              other[f][x] = read_8<T, kWords>(at + x * 8, out_cols - my_j - x * 8);
+              if constexpr (kOp == kMoeDx && kEnd == kEndSwiglu) pair[f][x] = read_8<T, kWords>(at + x * 8 + p.n_j, out_cols - my_j - x * 8);
             });
           });
+          loads_arrived();
         }
         fence();
-        each<2>([&](auto ff) {
-          constexpr int f = decltype(fs)::value * 2 + decltype(ff)::value;
-          const int64_t i = done.first + my_row + 16 * f;
+        each<kAtOnce>([&](auto ff) {
+          constexpr int f = decltype(fs)::value * kAtOnce + decltype(ff)::value;
+          const int64_t i = done.first + my_row + kRowApart * f;
           float v[16];
-          each<16>([&](auto x) { v[x] = acc[f][x / 4][x % 4]; });
+          // (float32 columns across: the four of a lane are those of its four fragments)
+          each<16>([&](auto nth) {
+            constexpr int x = decltype(nth)::value;
+            v[x] = k16 || kBAlongR ? acc[f][x / 4][x % 4] : acc[f][x % 4][x / 4];
+          });
           if (i >= done.end) return;
           if constexpr (kGated) {
-            if (my_j < out_cols) moe_emit_gated_8<T>(p, i, my_j, v, v + 8, bias[0], bias[1], other[ff][0]);
+            if (my_j >= out_cols) return;
+            moe_emit_gated_8<T, kWords>(p, i, my_j, out_cols - my_j, v, v + 8, bias[0], bias[1], other[ff][0]);
           } else {
             each<2>([&](auto x) {
-              if (my_j + x * 8 < out_cols) moe_emit_8<T, kOp, kEnd>(p, act, done.expert, i, my_j + x * 8, v + x * 8, bias[x], other[ff][x], pair[ff][x]);
+              const int32_t j = my_j + x * 8;
+              if (j >= out_cols) return;
+              moe_emit_8<T, kOp, kEnd, kWords>(p, act, done.expert, i, j, out_cols - j, v + x * 8, bias[x], other[ff][x], pair[ff][x]);
             });
           }
         });
         fence();
       });
+    }
+    if constexpr (kSumZ) {
+      if (done_sum_z && my_q == 0) {
+        each<2>([&](auto f) {
+          const int64_t i = done.first + my_row + kRowApart * (wn * 2 + f);
+          if (i < done.end) ((T*)p.db)[done.expert * p.db_stride + i] = from_float<T>(acc_z[f][0]);
+        });
+      }
     }
     stored = !none && done.first + S::kBM <= done.end && done_j0 + kColsC <= out_cols;
     if (!more) return;
@@ -380,8 +496,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
 
 // Two shapes of tiles.  Wide ones read LDS least for a matrix instruction, but come in few and one workgroup fills a CU; of
 // the others a CU holds two workgroups, and what is over at the ends of rows, experts and turns is a quarter.
-using Wide = Shape<256, 256, 2, 4, 64, 2, 1>;
-using Narrow = Shape<128, 128, 2, 2, 64, 2, 2>;
+using Wide = Shape<256, 256, 2, 4, 2, 1>;
+using Narrow = Shape<128, 128, 2, 2, 2, 2>;
 
 // Microseconds of a launch as measured for 64 of r and for the rest of a tile (8192 x 8192 x 8192 to 32768 x 2048 x 1024): what
 // decides between the shapes.  An expert's last tile is half full on average.
@@ -397,19 +513,22 @@ double estimate(const MoeProduct& p, int32_t out_cols, int32_t cols) {
     tiles = j_tiles * (p.expert_ptr ? std::min(rows, rows / S::kBM + 0.5 * p.n_experts) : (double)((p.n_rows + S::kBM - 1) / S::kBM));
     r = p.n_r;
   }
-  return std::ceil(tiles / (256 * S::kGroups)) * (std::ceil(r / 64) * per_64 + per_tile);
+  const double turns = std::ceil(tiles / (256 * S::kGroups)), us = turns * (std::ceil(r / 64) * per_64 + per_tile);
+  // (dw: experts differ in rows, the more so the fewer of them a workgroup sees; 32 experts of 1024 rows, 2048 x 1024: 4 turns of
+  // wide tiles 254 us, 8 of narrow ones 220)
+  return kOp == kMoeDw && p.expert_ptr ? us * (1 + 1.2 / turns) : us;
 }
 
-template <MoeOp kOp, typename S>
+template <MoeOp kOp, bool kWords, typename S>
 sptir_status_t launch(int32_t type, int32_t act, const MoeProduct& p, int32_t out_cols, int32_t cols, hipStream_t stream) {
-  const int64_t j_tiles = (out_cols + cols - 1) / cols;
+  const int64_t j_tiles = std::max((out_cols + cols - 1) / cols, kOp == kMoeDw && p.db ? 1 : 0);  // (db is summed beside dW's first columns)
   const int64_t i_tiles = kOp == kMoeDw ? (p.n_i + S::kBM - 1) / S::kBM : moe_most_tiles(p.n_rows, p.n_experts, p.expert_ptr, S::kBM);
   const int64_t tiles = i_tiles * j_tiles * (kOp == kMoeDw ? p.n_experts : 1);
   if (tiles == 0) return SPTIR_OK;
   if (tiles > (int64_t)INT32_MAX) return SPTIR_ERR_OVERFLOW;
   const int64_t groups = std::min<int64_t>(tiles, (int64_t)256 * S::kGroups);  // those that run at once
   auto go = [&](auto v, auto end) {
-    auto* kernel = k_moe_tiles<decltype(v), kOp, decltype(end)::value, S>;
+    auto* kernel = k_moe_tiles<decltype(v), kOp, decltype(end)::value, kWords, S>;
     static OncePerDevice allowed;
     allow_dynamic_lds((const void*)kernel, S::kLds, allowed);
     hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(S::kThreads), S::kLds, stream, p, act, (int32_t)j_tiles, (int32_t)i_tiles);
@@ -418,11 +537,14 @@ sptir_status_t launch(int32_t type, int32_t act, const MoeProduct& p, int32_t ou
     if constexpr (kOp != kMoeDw) {
       if (act == SPTIR_ACT_SWIGLU) return go(v, std::integral_constant<MoeEnd, kEndSwiglu>{});
       if (act != SPTIR_ACT_NONE) return go(v, std::integral_constant<MoeEnd, kEndAct>{});
+    } else if (p.db) {
+      return go(v, std::integral_constant<MoeEnd, kEndAct>{});
     }
     go(v, std::integral_constant<MoeEnd, kEndNone>{});
   };
   if (type == SPTIR_F16) with(_Float16{});
-  else with(__bf16{});
+  else if (type == SPTIR_BF16) with(__bf16{});
+  else if constexpr (S::kBM == 128) with(float{});
   SPTIR_HIP(hipGetLastError());
   return SPTIR_OK;
 }
@@ -434,24 +556,33 @@ template <MoeOp kOp>
 int32_t columns(int32_t act, const MoeProduct& p) { return kOp == kMoeForward && act == SPTIR_ACT_SWIGLU ? p.n_j / 2 : p.n_j; }
 
 template <MoeOp kOp>
-sptir_status_t launch_best(int32_t type, int32_t act, const MoeProduct& p, hipStream_t stream) {
+sptir_status_t launch_best(int32_t type, int32_t act, bool words, const MoeProduct& p, hipStream_t stream) {
   const int32_t out_cols = columns<kOp>(act, p), wide = columns<kOp, Wide>(act), narrow = columns<kOp, Narrow>(act);
-  if (estimate<kOp, Wide>(p, out_cols, wide) < estimate<kOp, Narrow>(p, out_cols, narrow))
-    return launch<kOp, Wide>(type, act, p, out_cols, wide, stream);
-  return launch<kOp, Narrow>(type, act, p, out_cols, narrow, stream);
+  if (!words) return launch<kOp, false, Narrow>(type, act, p, out_cols, narrow, stream);
+  if (type != SPTIR_F32 && estimate<kOp, Wide>(p, out_cols, wide) < estimate<kOp, Narrow>(p, out_cols, narrow))
+    return launch<kOp, true, Wide>(type, act, p, out_cols, wide, stream);
+  return launch<kOp, true, Narrow>(type, act, p, out_cols, narrow, stream);
 }
 
 }  // namespace
 
-double moe_tiles_forward_estimate(int32_t act, const MoeProduct& p) {
+double moe_tiles_forward_estimate(int32_t type, int32_t act, bool words, const MoeProduct& p) {
   const int32_t out_cols = columns<kMoeForward>(act, p);
-  const double us = std::min(estimate<kMoeForward, Wide>(p, out_cols, columns<kMoeForward, Wide>(act)),
-                             estimate<kMoeForward, Narrow>(p, out_cols, columns<kMoeForward, Narrow>(act)));
+  double us = estimate<kMoeForward, Narrow>(p, out_cols, columns<kMoeForward, Narrow>(act));
+  if (type == SPTIR_F32) us *= 6.5;
+  else if (!words) us *= 1.5;
+  else us = std::min(us, estimate<kMoeForward, Wide>(p, out_cols, columns<kMoeForward, Wide>(act)));
   // ... and no less than the weights take from memory
-  return std::max(us, (double)std::min<int64_t>(p.n_rows, p.n_experts) * p.n_j * p.n_r * 2 / 4.1e6);
+  return std::max(us, (double)std::min<int64_t>(p.n_rows, p.n_experts) * p.n_j * p.n_r * moe_type_bytes(type) / 4.1e6);
 }
-sptir_status_t moe_tiles_forward(int32_t type, int32_t act, const MoeProduct& p, hipStream_t stream) { return launch_best<kMoeForward>(type, act, p, stream); }
-sptir_status_t moe_tiles_dx(int32_t type, int32_t act, const MoeProduct& p, hipStream_t stream) { return launch_best<kMoeDx>(type, act, p, stream); }
-sptir_status_t moe_tiles_dw(int32_t type, const MoeProduct& p, hipStream_t stream) { return launch_best<kMoeDw>(type, SPTIR_ACT_NONE, p, stream); }
+sptir_status_t moe_tiles_forward(int32_t type, int32_t act, bool words, const MoeProduct& p, hipStream_t stream) {
+  return launch_best<kMoeForward>(type, act, words, p, stream);
+}
+sptir_status_t moe_tiles_dx(int32_t type, int32_t act, bool words, const MoeProduct& p, hipStream_t stream) {
+  return launch_best<kMoeDx>(type, act, words, p, stream);
+}
+sptir_status_t moe_tiles_dw(int32_t type, bool words, const MoeProduct& p, hipStream_t stream) {
+  return launch_best<kMoeDw>(type, SPTIR_ACT_NONE, words, p, stream);
+}
 
 }  // namespace sptir
