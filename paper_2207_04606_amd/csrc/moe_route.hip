@@ -213,9 +213,13 @@ __global__ __launch_bounds__(1024) void k_moe_count(const int32_t* __restrict__ 
   for (int e = threadIdx.x; e < n_experts; e += blockDim.x) count[e] = 0;
   __syncthreads();
   const int64_t lo = blockIdx.x * part, hi = min(n, lo + part);
-  for (int64_t i = lo + threadIdx.x; i < hi; i += blockDim.x) {
-    const int e = experts[i];
-    if (e >= 0 && e < n_experts) atomicAdd(&count[e], 1);
+  const int lane = threadIdx.x & 63, bits = 32 - __clz(n_experts);
+  for (int64_t i0 = lo + (threadIdx.x & ~63); i0 < hi; i0 += blockDim.x) {
+    int e = i0 + lane < hi ? experts[i0 + lane] : -1;
+    if (e < 0 || e > n_experts) e = n_experts;
+    // (a lane adds for all that name its expert: an LDS atomic takes a turn for every lane with the same address)
+    const unsigned long long same = lanes_alike(e, bits);
+    if (e < n_experts && (same & ((1ull << lane) - 1)) == 0) atomicAdd(&count[e], __popcll(same));
   }
   __syncthreads();
   for (int e = threadIdx.x; e < n_experts; e += blockDim.x) counts[(int64_t)blockIdx.x * n_experts + e] = count[e];
@@ -238,37 +242,55 @@ __global__ __launch_bounds__(1024) void k_moe_place(const int32_t* __restrict__ 
     const int e = i < w_hi ? experts[i] : -1;
     return e >= 0 && e < n_experts ? e : n_experts;
   };
+  const int bits = 32 - __clz(n_experts);  // (n_experts itself stands for "dropped")
   int held[kHeld];
 #pragma unroll
   for (int h = 0; h < kHeld; ++h) held[h] = w_lo + 64 * h < w_hi ? expert_at(w_lo + 64 * h + lane) : n_experts;
   for (int i = threadIdx.x; i < (waves + 2) * n_experts; i += blockDim.x) place[i] = 0;
   __syncthreads();
+  // Counts a turn: the lowest lane of an expert adds for all.  Returns the lane's rank among them and their number.
+  auto count = [&](int e) {
+    const unsigned long long same = lanes_alike(e, bits);
+    const int rank = __popcll(same & ((1ull << lane) - 1)), many = __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+    if (e < n_experts && rank == 0) mine[e] += many;
+    __builtin_amdgcn_wave_barrier();
+    return rank | many << 8;
+  };
 #pragma unroll
   for (int h = 0; h < kHeld; ++h)
-    if (held[h] < n_experts) atomicAdd(&mine[held[h]], 1);
-  for (int64_t i = w_lo + 64 * kHeld + lane; i < w_hi; i += 64) {
-    const int e = expert_at(i);
-    if (e < n_experts) atomicAdd(&mine[e], 1);
-  }
-  if (counts) {  // (whole numbers: the order of these sums changes nothing)
-    const int many = (int)gridDim.x * n_experts, own = (int)blockIdx.x * n_experts;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < many; i += blockDim.x) {
-      const int c = counts[i];
-      if (c) {
-        atomicAdd(&total[i % n_experts], c);
-        if (i < own) atomicAdd(&before[i % n_experts], c);
+    if (w_lo + 64 * h < w_hi) held[h] |= count(held[h]) << 16;  // (an expert has 11 bits)
+  for (int64_t i0 = w_lo + 64 * kHeld; i0 < w_hi; i0 += 64) count(expert_at(i0 + lane));
+  if (counts) {  // a thread per expert, or several that share its workgroups (whole numbers: their order changes nothing)
+    const int threads = blockDim.x, share = max(1, threads / n_experts);
+    for (int e0 = 0; e0 < n_experts; e0 += threads) {
+      const int e = n_experts <= threads ? (int)threadIdx.x % n_experts : e0 + (int)threadIdx.x;
+      const int g0 = n_experts <= threads ? (int)threadIdx.x / n_experts : 0;
+      if (e >= n_experts || g0 >= share) continue;
+      int all = 0, own = 0;
+#pragma unroll 8
+      for (int g = g0; g < (int)gridDim.x; g += share) {
+        const int c = counts[(int64_t)g * n_experts + e];
+        all += c;
+        own += g < (int)blockIdx.x ? c : 0;
       }
+      atomicAdd(&total[e], all);
+      atomicAdd(&before[e], own);
     }
   }
   __syncthreads();
   // an expert's first places inside the workgroup, and without other workgroups its total
   for (int e = threadIdx.x; e < n_experts; e += blockDim.x) {
     int at = before[e];
-    for (int w = 0; w < waves; ++w) {
-      const int c = place[w * n_experts + e];
-      place[w * n_experts + e] = at;
-      at += c;
+    for (int w0 = 0; w0 < waves; w0 += 4) {  // (waves is a multiple of 4: four reads at once)
+      int c[4];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) c[w] = place[(w0 + w) * n_experts + e];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        place[(w0 + w) * n_experts + e] = at;
+        at += c[w];
+      }
     }
     if (!counts) total[e] = at;
   }
@@ -291,21 +313,18 @@ __global__ __launch_bounds__(1024) void k_moe_place(const int32_t* __restrict__ 
       running += wave_total[w];
     }
     if (e < n_experts) {
-      const int first = base + s - c;
-      if (blockIdx.x == 0) expert_ptr[e] = first;
-      for (int w = 0; w < waves; ++w) place[w * n_experts + e] += first;
+      total[e] = base + s - c;
+      if (blockIdx.x == 0) expert_ptr[e] = total[e];
     }
     __syncthreads();
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) expert_ptr[n_experts] = running;
-  const int bits = 32 - __clz(n_experts);  // (n_experts itself stands for "dropped")
-  auto put = [&](int64_t i, int e) {
-    const unsigned long long same = lanes_alike(e, bits);
-    const int rank = __popcll(same & ((1ull << lane) - 1));
+  auto put = [&](int64_t i, int e, int ranked) {
+    const int rank = ranked & 0xff;
     int slot = -1;
-    if (e < n_experts) slot = mine[e] + rank;
+    if (e < n_experts) slot = total[e] + mine[e] + rank;
     __builtin_amdgcn_wave_barrier();
-    if (e < n_experts && rank == 0) mine[e] += __popcll(same);
+    if (e < n_experts && rank == 0) mine[e] += ranked >> 8;
     __builtin_amdgcn_wave_barrier();
     if (i < w_hi) {
       slot_of[i] = slot;
@@ -314,18 +333,23 @@ __global__ __launch_bounds__(1024) void k_moe_place(const int32_t* __restrict__ 
   };
 #pragma unroll
   for (int h = 0; h < kHeld; ++h)
-    if (w_lo + 64 * h < w_hi) put(w_lo + 64 * h + lane, held[h]);
-  for (int64_t i0 = w_lo + 64 * kHeld; i0 < w_hi; i0 += 64) put(i0 + lane, expert_at(i0 + lane));
+    if (w_lo + 64 * h < w_hi) put(w_lo + 64 * h + lane, held[h] & 0xffff, (unsigned)held[h] >> 16);
+  for (int64_t i0 = w_lo + 64 * kHeld; i0 < w_hi; i0 += 64) {
+    const int e = expert_at(i0 + lane);
+    const unsigned long long same = lanes_alike(e, bits);
+    put(i0 + lane, e, __popcll(same & ((1ull << lane) - 1)) | __popcll(same) << 8);
+  }
   for (int64_t s = running + (int64_t)blockIdx.x * blockDim.x + threadIdx.x; s < n; s += (int64_t)gridDim.x * blockDim.x)
     entry_of[s] = -1;
 }
 
-// entries of a workgroup: one workgroup up to 16 K (a launch less), then at most 128 workgroups (each adds up the counts of all)
-constexpr int64_t kSortAlone = 16384, kSortPart = 4096;
-constexpr int kSortGroups = 128;
-int64_t sort_part(int64_t n) {
+// Entries of a workgroup: one workgroup up to 2 K of them (a launch less), then 1 K each, more where all workgroups' counts, which
+// every one adds up, would be more than 32 K.
+constexpr int64_t kSortAlone = 2048, kSortPart = 1024, kSortCounts = 32768;
+int64_t sort_part(int64_t n, int32_t n_experts) {
   if (n <= kSortAlone) return std::max<int64_t>(n, 1);
-  return std::max<int64_t>(kSortPart, ((n + kSortGroups - 1) / kSortGroups + 63) / 64 * 64);
+  const int64_t groups = std::max<int64_t>(32, kSortCounts / n_experts);
+  return std::max<int64_t>(kSortPart, ((n + groups - 1) / groups + 63) / 64 * 64);
 }
 
 }  // namespace
@@ -379,7 +403,7 @@ extern "C" sptir_status_t sptir_moe_route_backward(const void* logits, int32_t t
 
 extern "C" int64_t sptir_moe_sort_workspace(int64_t n_entries, int32_t n_experts) {
   if (n_entries <= kSortAlone || n_experts < 1) return 0;
-  const int64_t part = sort_part(n_entries);
+  const int64_t part = sort_part(n_entries, n_experts);
   return (n_entries + part - 1) / part * n_experts * (int64_t)sizeof(int32_t);
 }
 
@@ -392,10 +416,10 @@ extern "C" sptir_status_t sptir_moe_sort(const int32_t* experts, int32_t n_token
   if (!expert_ptr || (n > 0 && (!experts || !entry_of || !slot_of))) return SPTIR_ERR_INVALID_ARG;
   const int64_t need = sptir_moe_sort_workspace(n, n_experts);
   if (need > 0 && (!workspace || workspace_bytes < need)) return SPTIR_ERR_INVALID_ARG;
-  const int64_t part = sort_part(n);
+  const int64_t part = sort_part(n, n_experts);
   const int groups = (int)std::max<int64_t>(1, (n + part - 1) / part);
   // 16 wavefronts, fewer where there is less for them than 64 entries each
-  const int waves = (int)std::min<int64_t>(16, std::max<int64_t>(4, (part + 63) / 64));
+  const int waves = (int)std::min<int64_t>(16, std::max<int64_t>(4, (part + 255) / 256 * 4));
   if (groups > 1)
     hipLaunchKernelGGL(k_moe_count, dim3(groups), dim3(1024), n_experts * sizeof(int32_t), (hipStream_t)stream, experts, n, part,
                        n_experts, (int32_t*)workspace);
