@@ -36,6 +36,7 @@ struct MoeProduct {
   int64_t ldc, c_stride;
   void* db;                   // dw: sums of dZ over an expert's rows; may be NULL
   int64_t db_stride;
+  int32_t parts;              // dw: an expert's rows are taken in so many (more than 1: C and db are the workspace's)
 };
 
 // The rows of an m-tile: tiles of `rows` rows, an expert's last one ragged; the rows behind the last expert's are a group of

@@ -87,12 +87,15 @@ extern "C" sptir_status_t sptir_moe_product_dx(const sptir_moe_routing_t* routin
   p.B = q->W; p.ldb = q->ldw; p.b_stride = p.n_experts > 1 ? q->w_stride : 0;
   p.pre = const_cast<void*>(q->pre); p.ld_pre = q->ld_pre;
   p.C = q->dX; p.ldc = q->ld_dx;
-  const bool words = moe_near(q->type, p.n_rows, p.lda) && moe_words(q->type, q->d_z, {p.A}, {p.lda}) &&
+  const bool words = moe_near(q->type, p.n_rows, p.lda) && moe_near(q->type, kMoeStep, p.ldb) && moe_words(q->type, q->d_z, {p.A}, {p.lda}) &&
                      moe_words(q->type, q->d_in, {p.B, act ? p.pre : nullptr, p.C}, {p.ldb, p.b_stride, act ? p.ld_pre : 0, p.ldc});
   return moe_tiles_dx(q->type, q->activation, words, p, (hipStream_t)stream);
 }
 
-extern "C" int64_t sptir_moe_product_dw_workspace(int64_t, int32_t, int32_t, int32_t) { return 0; }
+extern "C" int64_t sptir_moe_product_dw_workspace(int64_t n_rows, int32_t n_experts, int32_t d_in, int32_t d_z) {
+  if (n_rows <= 0 || n_experts <= 0 || d_in < 0 || d_z <= 0) return 0;
+  return moe_tiles_dw_workspace(moe_tiles_dw_parts(n_rows, n_experts, d_in, d_z), n_experts, d_in, d_z);
+}
 
 extern "C" sptir_status_t sptir_moe_product_dw(const sptir_moe_routing_t* routing, const sptir_moe_product_dw_t* q, void* stream) {
   if (!q || q->struct_size != (int32_t)sizeof(*q) || !moe_type_ok(q->type) || q->d_in < 0 || q->d_z < 0) return SPTIR_ERR_INVALID_ARG;
@@ -104,7 +107,7 @@ extern "C" sptir_status_t sptir_moe_product_dw(const sptir_moe_routing_t* routin
       (q->db && p.n_experts > 1 && q->db_stride < q->d_z))
     return SPTIR_ERR_INVALID_ARG;
   const int64_t need = sptir_moe_product_dw_workspace(q->n_rows, p.n_experts, q->d_in, q->d_z);
-  if (need > 0 && (!q->workspace || q->workspace_bytes < need)) return SPTIR_ERR_INVALID_ARG;
+  if (need > 0 && (!q->workspace || q->workspace_bytes < need || ((uintptr_t)q->workspace & 15))) return SPTIR_ERR_INVALID_ARG;
   if (q->d_z == 0) return SPTIR_OK;
   if ((q->d_in > 0 && !q->dW) || (q->n_rows > 0 && (!q->dZ || (q->d_in > 0 && !q->X))) || (q->dW && (q->dW == q->dZ || q->dW == q->X)) ||
       (q->db && (q->db == q->dZ || q->db == q->X || q->db == q->dW)))
@@ -114,6 +117,7 @@ extern "C" sptir_status_t sptir_moe_product_dw(const sptir_moe_routing_t* routin
   p.B = q->X; p.ldb = q->ldx;
   p.C = q->dW; p.ldc = q->ld_dw; p.c_stride = p.n_experts > 1 ? q->dw_stride : 0;
   p.db = q->db; p.db_stride = p.n_experts > 1 ? q->db_stride : 0;
-  const bool words = q->d_in > 0 && moe_words(q->type, q->d_z, {p.A}, {p.lda}) && moe_words(q->type, q->d_in, {p.B, p.C}, {p.ldb, p.ldc, p.c_stride});
-  return moe_tiles_dw(q->type, words, p, (hipStream_t)stream);
+  const bool words = q->d_in > 0 && moe_near(q->type, kMoeStep, p.lda) && moe_words(q->type, q->d_z, {p.A}, {p.lda}) &&
+                     moe_words(q->type, q->d_in, {p.B, p.C}, {p.ldb, p.ldc, p.c_stride});
+  return moe_tiles_dw(q->type, words, p, q->workspace, (hipStream_t)stream);
 }

@@ -22,12 +22,13 @@ __device__ inline void moe_square(uint32_t id, uint32_t rows, uint32_t cols, int
   *col = in / high;
 }
 
-// The experts' m-tiles, in LDS for as long as a workgroup runs: an expert's rows begin at `row` and its tiles end before
-// `last`; number n_experts are the rows of no expert.  One wavefront fills it in.  Returns the number of m-tiles.
+// The experts' m-tiles, in LDS for as long as a workgroup runs: an expert's rows begin at row[e] and its tiles end before
+// last[e]; number n_experts are the rows of no expert.  One wavefront fills it in.  Returns the number of m-tiles.
 struct MoeTable {
-  int32_t row[kMoeMaxExperts + 2], last[kMoeMaxExperts + 1];
+  int32_t *row, *last;  // [n_experts + 2], [n_experts + 1]
 };
-__device__ inline uint32_t moe_fill_table(const MoeProduct& p, int rows, MoeTable* table) {
+inline int moe_table_bytes(const int32_t* expert_ptr, int32_t n_experts) { return expert_ptr ? (2 * n_experts + 3) * (int)sizeof(int32_t) : 0; }
+__device__ inline uint32_t moe_fill_table(const MoeProduct& p, int rows, const MoeTable& table) {
   if (!p.expert_ptr) return (uint32_t)((p.n_rows + rows - 1) / rows);
   if (threadIdx.x < 64) {
     int before = 0;
@@ -43,17 +44,17 @@ __device__ inline uint32_t moe_fill_table(const MoeProduct& p, int rows, MoeTabl
         if ((int)threadIdx.x >= d) sum += o;
       }
       if (e <= p.n_experts) {
-        table->row[e] = lo;
-        table->last[e] = before + sum;
+        table.row[e] = lo;
+        table.last[e] = before + sum;
       }
       before += __shfl(sum, 63);
     }
-    if (threadIdx.x == 0) table->row[p.n_experts + 1] = (int)p.n_rows;
+    if (threadIdx.x == 0) table.row[p.n_experts + 1] = (int)p.n_rows;
   }
   __syncthreads();
-  return (uint32_t)__builtin_amdgcn_readfirstlane(table->last[p.n_experts]);
+  return (uint32_t)__builtin_amdgcn_readfirstlane(table.last[p.n_experts]);
 }
-__device__ inline void moe_look_up(const MoeProduct& p, int rows, int tile, const MoeTable* table, MoeTile* out) {
+__device__ inline void moe_look_up(const MoeProduct& p, int rows, int tile, const MoeTable& table, MoeTile* out) {
   if (!p.expert_ptr) {
     *out = {0, (int64_t)tile * rows, p.n_rows};
     return;
@@ -61,15 +62,15 @@ __device__ inline void moe_look_up(const MoeProduct& p, int rows, int tile, cons
   int e = 0;  // the first whose tiles end behind this one
   for (int e0 = 0; e0 <= p.n_experts; e0 += 64) {
     const int at = e0 + (int)(threadIdx.x & 63);
-    const unsigned long long past = __ballot(at <= p.n_experts && table->last[at <= p.n_experts ? at : 0] > tile);
+    const unsigned long long past = __ballot(at <= p.n_experts && table.last[at <= p.n_experts ? at : 0] > tile);
     if (past) {
       e = e0 + __ffsll(past) - 1;
       break;
     }
   }
-  const int begin = e > 0 ? table->last[e - 1] : 0, row = table->row[e];
+  const int begin = e > 0 ? table.last[e - 1] : 0, row = table.row[e];
   *out = {__builtin_amdgcn_readfirstlane(e), __builtin_amdgcn_readfirstlane(row) + (int64_t)(tile - __builtin_amdgcn_readfirstlane(begin)) * rows,
-          __builtin_amdgcn_readfirstlane(table->row[e + 1])};
+          __builtin_amdgcn_readfirstlane(table.row[e + 1])};
 }
 
 // ---- eight elements at a time, of which there are `many`; kWords: they lie in 16-byte words, and whole words of them are there
@@ -132,8 +133,9 @@ __device__ inline void add_8(float (&v)[8], const Eight<T>& w) {
   for (int i = 0; i < 8; ++i) v[i] += w.at(i);
 }
 
-// what comes after the sums: nothing, an activation of one column (dw: the sums of dZ as well), swiglu's pairs
-enum MoeEnd { kEndNone, kEndAct, kEndSwiglu };
+// what comes after the sums: nothing, an activation of one column (dw: the sums of dZ as well), swiglu's pairs; dw: sums of
+// parts of the rows, without and with those of dZ
+enum MoeEnd { kEndNone, kEndAct, kEndSwiglu, kEndParts, kEndPartsSum };
 
 // Eight columns of a row of C from the sums: `bias` and `other` (forward: the residual; dx: z of the product before) have been
 // read by the caller, together for many rows.
@@ -168,6 +170,8 @@ __device__ inline void moe_emit_8(const MoeProduct& p, int32_t act, int expert, 
       write_8<T, kWords>((T*)p.C + i * p.ldc + j + p.n_j, many, du);
     }
     write_8<T, kWords>((T*)p.C + i * p.ldc + j, many, v);
+  } else if constexpr (kEnd >= kEndParts) {
+    write_8<float, true>((float*)p.C + expert * p.c_stride + i * p.ldc + j, many, v);
   } else {
     write_8<T, kWords>((T*)p.C + expert * p.c_stride + i * p.ldc + j, many, v);
   }
@@ -202,18 +206,21 @@ __device__ inline void moe_clear_8(const MoeProduct& p, int64_t i, int32_t j, in
   if (kOp == kMoeDx && kEnd == kEndSwiglu) write_8<T, kWords>((T*)p.C + i * p.ldc + j + p.n_j, many, zero);
 }
 
-// the tiles' kernels count 16-byte words of an operand with 32 bits
+constexpr int kMoeStep = 64;  // most of r that a step takes
+// the tiles' kernels count 16-byte words of an operand (of a step's lines, where they lie across) with 32 bits
 inline bool moe_near(int32_t type, int64_t rows, int64_t ld) {
   return rows == 0 || ld < ((int64_t)1 << 32) * (16 / moe_type_bytes(type)) / rows;
 }
 
-// ---- launches (moe_few.hip, moe_tiles.hip; words: in 16-byte words throughout)
+// ---- launches (moe_few.hip, moe_tiles_*.hip; words: in 16-byte words throughout)
 double moe_few_estimate(int32_t type, const MoeProduct& p, int32_t* fragments);  // microseconds
 sptir_status_t moe_few_forward(int32_t type, int32_t act, const MoeProduct& p, int32_t fragments, hipStream_t stream);
 double moe_tiles_forward_estimate(int32_t type, int32_t act, bool words, const MoeProduct& p);
 sptir_status_t moe_tiles_forward(int32_t type, int32_t act, bool words, const MoeProduct& p, hipStream_t stream);
 sptir_status_t moe_tiles_dx(int32_t type, int32_t act, bool words, const MoeProduct& p, hipStream_t stream);
-sptir_status_t moe_tiles_dw(int32_t type, bool words, const MoeProduct& p, hipStream_t stream);
+int32_t moe_tiles_dw_parts(int64_t n_rows, int32_t n_experts, int32_t d_in, int32_t d_z);  // (of an expert's rows)
+int64_t moe_tiles_dw_workspace(int32_t parts, int32_t n_experts, int32_t d_in, int32_t d_z);
+sptir_status_t moe_tiles_dw(int32_t type, bool words, const MoeProduct& p, void* workspace, hipStream_t stream);
 
 }  // namespace sptir
 

@@ -1,4 +1,8 @@
-// The experts' products in large tiles: operands from memory to LDS, matrix instructions from there.
+// The experts' products in tiles: operands from memory to LDS, matrix instructions from there.  (Compiled once for every
+// product, moe_tiles_forward.hip, moe_tiles_dx.hip and moe_tiles_dw.hip.)
+#ifndef SPTIR_MOE_TILES_KERNEL_H_
+#define SPTIR_MOE_TILES_KERNEL_H_
+
 #include <algorithm>
 #include <cmath>
 #include <utility>
@@ -18,17 +22,16 @@ __device__ inline void to_lds(const void* from, lds_char* to) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
-// A step takes 128 bytes of r: 64 elements of 16 bits, 32 of float32.  kStages: steps that LDS holds.
-template <int kBM_, int kBN_, int kWavesM_, int kWavesN_, int kStages_, int kGroups_>
+// A step takes 128 bytes of r: 64 elements of 16 bits, 32 of float32.  LDS holds two of them.
+template <int kBM_, int kBN_, int kWavesM_, int kWavesN_, int kGroups_>
 struct Shape {
-  static constexpr int kBM = kBM_, kBN = kBN_, kWavesM = kWavesM_, kWavesN = kWavesN_, kStages = kStages_;
+  static constexpr int kBM = kBM_, kBN = kBN_, kWavesM = kWavesM_, kWavesN = kWavesN_;
   static constexpr int kGroups = kGroups_;  // workgroups that a CU holds
   static constexpr int kThreads = 64 * kWavesM * kWavesN, kWavesPerSimd = kGroups * kThreads / 256;
   static constexpr int kFM = kBM / kWavesM / 16, kFN = kBN / kWavesN / 16;  // fragments of a wavefront's tile
   static_assert(kFN == 4, "a wavefront has 64 columns");
   static constexpr int kBytesA = kBM * 128, kBytesB = kBN * 128, kStage = kBytesA + kBytesB;
-  static constexpr int kLds = kStages * kStage + (int)sizeof(MoeTable);
-  static_assert(kGroups * kLds <= 160 * 1024, "LDS");
+  static_assert(kGroups * (2 * kStage + 2 * 1024) <= 160 * 1024, "LDS, with the table of 250 experts");
 };
 
 // Which 16-byte chunk of a line lies at place `pos` of it in LDS: pos ^ key(line), so that the lanes that read together find
@@ -99,9 +102,9 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
 
   // ---- the tiles of this workgroup
   const uint32_t per_expert = (uint32_t)i_tiles * j_tiles;
-  MoeTable* table = (MoeTable*)(lds_generic + S::kStages * S::kStage);
+  const MoeTable table = {(int32_t*)(lds_generic + 2 * S::kStage), (int32_t*)(lds_generic + 2 * S::kStage) + p.n_experts + 2};
   const uint32_t m_tiles = kOp == kMoeDw ? 0 : moe_fill_table(p, S::kBM, table);
-  const uint32_t total = kOp == kMoeDw ? per_expert * p.n_experts : m_tiles * j_tiles;
+  const uint32_t total = kOp == kMoeDw ? per_expert * p.n_experts * (kEnd >= kEndParts ? p.parts : 1) : m_tiles * j_tiles;
   MoeTile t;
   int32_t j0;
   int64_t r0 = 0, r1 = p.n_r;
@@ -128,18 +131,24 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   u32x4 held[kHeld];
   const int64_t a_step = (kAAlongR ? kBR : kBR * p.lda) * (int64_t)sizeof(T), b_step = (kBAlongR ? kBR : kBR * p.ldb) * (int64_t)sizeof(T);
 
-  constexpr bool kSumZ = kOp == kMoeDw && kEnd != kEndNone;  // (db is asked for)
+  constexpr bool kParts = kEnd == kEndParts || kEnd == kEndPartsSum;  // (dw: sums of parts of an expert's rows, in float32)
+  constexpr bool kSumZ = kOp == kMoeDw && (kEnd == kEndAct || kEnd == kEndPartsSum);  // (db is asked for)
   bool sum_z = false;  // this tile's workgroup sums dZ too
   auto start = [&](uint32_t id) __attribute__((always_inline)) {
     const uint32_t dealt = moe_deal(id, total);
     int jt;
     if constexpr (kOp == kMoeDw) {
-      const int e = (int)(dealt / per_expert);
+      const int which = (int)(dealt / per_expert), e = kParts ? which % p.n_experts : which;
       int it;
       moe_square(dealt % per_expert, i_tiles, j_tiles, &it, &jt);
-      t = {e, (int64_t)it * S::kBM, p.n_i};
+      t = {which, (int64_t)it * S::kBM, p.n_i};
       r0 = p.expert_ptr ? p.expert_ptr[e] : 0;
       r1 = p.expert_ptr ? p.expert_ptr[e + 1] : p.n_rows;
+      if constexpr (kParts) {
+        const int64_t each = ((r1 - r0 + p.parts - 1) / p.parts + 63) / 64 * 64;
+        r0 = min(r0 + which / p.n_experts * each, r1);
+        r1 = min(r0 + each, r1);
+      }
       sum_z = kSumZ && jt == 0;
     } else {
       int mt;
@@ -257,9 +266,10 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   // ---- products
   using M = Mma<T>;
   using Frag = typename M::Frag;
-  f32x4 acc[S::kFM][S::kFN], acc_z[2];
+  constexpr int kZ = S::kFM / S::kWavesN;  // fragments of rows whose sums of dZ a wavefront has
+  f32x4 acc[S::kFM][S::kFN], acc_z[kSumZ ? kZ : 1];
   // A phase multiplies two fragments of rows with the columns', 64 bytes of r, while the fragments of the next phase are read.
-  constexpr int kPhases = S::kFM / 2, kParts = 2;
+  constexpr int kPhases = S::kFM / 2, kHalves = 2;
   static_assert(kPhases % 2 == 0, "the sets of fragments alternate");
   Frag a[2][2], b[2][S::kFN];
   auto read_rows = [&](int stage, int kk, auto phase) __attribute__((always_inline)) {
@@ -312,17 +322,19 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
       each<4>([&](auto g) { acc[ph * 2 + f][g] = M::run(b[kSet][g], a[ph & 1][f], acc[ph * 2 + f][g]); });
     });
     if constexpr (kSumZ) {  // dZ times ones: the wavefronts that share rows take a phase's each
-      if (sum_z && wn == ph) {
+      if (sum_z && wn == ph % S::kWavesN) {
         Frag ones;
         each<kN>([&](auto x) { ones[decltype(x)::value] = from_float<T>(1.f); });
-        each<2>([&](auto f) { acc_z[f] = M::run(ones, a[ph & 1][f], acc_z[f]); });
+        each<2>([&](auto f) {
+          constexpr int z = ph / S::kWavesN * 2 + decltype(f)::value;
+          acc_z[z] = M::run(ones, a[ph & 1][f], acc_z[z]);
+        });
       }
     }
   };
-  static_assert(kOp != kMoeDw || S::kWavesN == kPhases, "a wavefront for every phase");
 
   // One step.  The barrier before its last phase says that this step's part of LDS has been read and that the next step's is
-  // there; the loads of kStages - 2 more steps may still be on their way.  The order of a phase is kept as it is written
+  // there.  The order of a phase is kept as it is written
   // (fences): reads first, so that they arrive while the phase's matrix instructions run.
   using Set0 = std::integral_constant<int, 0>;
   // A whole tile's epilogue issues at least so many stores behind the next tile's first loads: these need not be waited for
@@ -331,9 +343,9 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   bool stored = false;
   int stage = 0;
   auto run_step = [&](int s) __attribute__((always_inline)) {
-    const int next = S::kStages == 2 ? stage ^ 1 : stage + 1 == S::kStages ? 0 : stage + 1;
-    each<kParts>([&](auto part) {
-      constexpr int kk = decltype(part)::value;
+    const int next = stage ^ 1;
+    each<kHalves>([&](auto half) {
+      constexpr int kk = decltype(half)::value;
       constexpr std::integral_constant<int, kk> set{};
       constexpr std::integral_constant<int, kk ^ 1> other{};
       each<kPhases - 1>([&](auto phase) {
@@ -343,26 +355,24 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
         fence();
       });
       constexpr std::integral_constant<int, kPhases - 1> last{};
-      if constexpr (kk + 1 < kParts) {
+      if constexpr (kk + 1 < kHalves) {
         read_cols(stage, kk + 1, other);
         read_rows(stage, kk + 1, Set0{});
         fence();
         multiply(set, last);
         fence();
       } else {
-        if (!kWords) arrive_and_meet<kNoWait>();
-        else if (S::kStages > 2 && s + S::kStages <= steps) arrive_and_meet<(S::kStages - 2) * kLoads>();
-        else arrive_and_meet<0>();
+        arrive_and_meet<kWords ? 0 : kNoWait>();
         if (s + 1 < steps) {
           read_cols(next, 0, other);
           read_rows(next, 0, Set0{});
         }
         fence();
         if constexpr (kWords) {
-          if (s + S::kStages < steps) load(s + S::kStages, stage);
+          if (s + 2 < steps) load(s + 2, stage);
         } else {
-          if (s + S::kStages < steps) put(s + S::kStages, stage);
-          if (s + S::kStages + 1 < steps) load(s + S::kStages + 1, 0);
+          if (s + 2 < steps) put(s + 2, stage);
+          if (s + 3 < steps) load(s + 3, 0);
         }
         multiply(set, last);
         fence();
@@ -375,7 +385,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
     stage = 0;
     ask(0);
     if constexpr (kWords) {
-      each<S::kStages>([&](auto s) { if (s < steps) load(s, s); });
+      each<2>([&](auto s) { if (s < steps) load(s, s); });
     } else {
       if (steps > 0) load(0, 0);
     }
@@ -386,19 +396,19 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   load_first();
   while (true) {
     each<S::kFM>([&](auto f) { each<S::kFN>([&](auto g) { acc[f][g] = f32x4{0.f, 0.f, 0.f, 0.f}; }); });
-    if (kSumZ) each<2>([&](auto f) { acc_z[f] = f32x4{0.f, 0.f, 0.f, 0.f}; });
+    if (kSumZ) each<kZ>([&](auto f) { acc_z[kSumZ ? (int)f : 0] = f32x4{0.f, 0.f, 0.f, 0.f}; });
     if (steps > 0) {
       if constexpr (!kWords) {
 #pragma unroll 1
-        for (int s = 0; s < S::kStages && s < steps; ++s) {
+        for (int s = 0; s < 2 && s < steps; ++s) {
           put(s, s);
           if (s + 1 < steps) load(s + 1, 0);
         }
         arrive_and_meet<kNoWait>();
-      } else if (stored && steps >= S::kStages) {
-        arrive_and_meet<(S::kStages - 1) * kLoads + kStores>();
-      } else if (steps >= S::kStages) {
-        arrive_and_meet<(S::kStages - 1) * kLoads>();
+      } else if (stored && steps >= 2) {
+        arrive_and_meet<kLoads + kStores>();
+      } else if (steps >= 2) {
+        arrive_and_meet<kLoads>();
       } else {
         arrive_and_meet<0>();
       }
@@ -483,9 +493,10 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
     }
     if constexpr (kSumZ) {
       if (done_sum_z && my_q == 0) {
-        each<2>([&](auto f) {
-          const int64_t i = done.first + my_row + kRowApart * (wn * 2 + f);
-          if (i < done.end) ((T*)p.db)[done.expert * p.db_stride + i] = from_float<T>(acc_z[f][0]);
+        each<kZ>([&](auto f) {
+          const int64_t i = done.first + my_row + kRowApart * ((f / 2 * S::kWavesN + wn) * 2 + f % 2);
+          using Sum = std::conditional_t<kParts, float, T>;
+          if (i < done.end) ((Sum*)p.db)[done.expert * p.db_stride + i] = from_float<Sum>(acc_z[f][0]);
         });
       }
     }
@@ -496,47 +507,48 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
 
 // Two shapes of tiles.  Wide ones read LDS least for a matrix instruction, but come in few and one workgroup fills a CU; of
 // the others a CU holds two workgroups, and what is over at the ends of rows, experts and turns is a quarter.
-using Wide = Shape<256, 256, 2, 4, 2, 1>;
-using Narrow = Shape<128, 128, 2, 2, 2, 2>;
+using Wide = Shape<256, 256, 2, 4, 1>;
+using Narrow = Shape<128, 128, 2, 2, 2>;
 
 // Microseconds of a launch as measured for 64 of r and for the rest of a tile (8192 x 8192 x 8192 to 32768 x 2048 x 1024): what
 // decides between the shapes.  An expert's last tile is half full on average.
+template <typename S>
+double tiles_us(double tiles, double r) {
+  const double per_64 = S::kBM == 256 ? 1.73 : 1.03, per_tile = S::kBM == 256 ? 5.0 : 2.0;
+  return std::ceil(tiles / (256 * S::kGroups)) * (std::ceil(r / 64) * per_64 + per_tile);
+}
 template <MoeOp kOp, typename S>
 double estimate(const MoeProduct& p, int32_t out_cols, int32_t cols) {
-  const double per_64 = S::kBM == 256 ? 1.73 : 1.03, per_tile = S::kBM == 256 ? 5.0 : 2.0;
   const double j_tiles = (out_cols + cols - 1) / cols, rows = (double)p.n_rows;
-  double tiles, r;
-  if (kOp == kMoeDw) {
-    tiles = j_tiles * ((p.n_i + S::kBM - 1) / S::kBM) * p.n_experts;
-    r = rows / p.n_experts;
-  } else {
-    tiles = j_tiles * (p.expert_ptr ? std::min(rows, rows / S::kBM + 0.5 * p.n_experts) : (double)((p.n_rows + S::kBM - 1) / S::kBM));
-    r = p.n_r;
-  }
-  const double turns = std::ceil(tiles / (256 * S::kGroups)), us = turns * (std::ceil(r / 64) * per_64 + per_tile);
-  // (dw: experts differ in rows, the more so the fewer of them a workgroup sees; 32 experts of 1024 rows, 2048 x 1024: 4 turns of
-  // wide tiles 254 us, 8 of narrow ones 220)
-  return kOp == kMoeDw && p.expert_ptr ? us * (1 + 1.2 / turns) : us;
+  const double m_tiles = p.expert_ptr ? std::min(rows, rows / S::kBM + 0.5 * p.n_experts) : (double)((p.n_rows + S::kBM - 1) / S::kBM);
+  return tiles_us<S>(j_tiles * m_tiles, p.n_r);
 }
 
 template <MoeOp kOp, bool kWords, typename S>
 sptir_status_t launch(int32_t type, int32_t act, const MoeProduct& p, int32_t out_cols, int32_t cols, hipStream_t stream) {
   const int64_t j_tiles = std::max((out_cols + cols - 1) / cols, kOp == kMoeDw && p.db ? 1 : 0);  // (db is summed beside dW's first columns)
   const int64_t i_tiles = kOp == kMoeDw ? (p.n_i + S::kBM - 1) / S::kBM : moe_most_tiles(p.n_rows, p.n_experts, p.expert_ptr, S::kBM);
-  const int64_t tiles = i_tiles * j_tiles * (kOp == kMoeDw ? p.n_experts : 1);
+  const int64_t tiles = i_tiles * j_tiles * (kOp == kMoeDw ? (int64_t)p.n_experts * p.parts : 1);
   if (tiles == 0) return SPTIR_OK;
   if (tiles > (int64_t)INT32_MAX) return SPTIR_ERR_OVERFLOW;
   const int64_t groups = std::min<int64_t>(tiles, (int64_t)256 * S::kGroups);  // those that run at once
   auto go = [&](auto v, auto end) {
     auto* kernel = k_moe_tiles<decltype(v), kOp, decltype(end)::value, kWords, S>;
     static OncePerDevice allowed;
-    allow_dynamic_lds((const void*)kernel, S::kLds, allowed);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(S::kThreads), S::kLds, stream, p, act, (int32_t)j_tiles, (int32_t)i_tiles);
+    const int lds = 2 * S::kStage + (kOp == kMoeDw ? 0 : moe_table_bytes(p.expert_ptr, p.n_experts));
+    allow_dynamic_lds((const void*)kernel, lds, allowed);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(S::kThreads), lds, stream, p, act, (int32_t)j_tiles, (int32_t)i_tiles);
   };
   auto with = [&](auto v) {
     if constexpr (kOp != kMoeDw) {
       if (act == SPTIR_ACT_SWIGLU) return go(v, std::integral_constant<MoeEnd, kEndSwiglu>{});
       if (act != SPTIR_ACT_NONE) return go(v, std::integral_constant<MoeEnd, kEndAct>{});
+    } else if (p.parts > 1) {
+      if constexpr (S::kBM <= 128) {
+        if (p.db) go(v, std::integral_constant<MoeEnd, kEndPartsSum>{});
+        else go(v, std::integral_constant<MoeEnd, kEndParts>{});
+      }
+      return;
     } else if (p.db) {
       return go(v, std::integral_constant<MoeEnd, kEndAct>{});
     }
@@ -544,7 +556,7 @@ sptir_status_t launch(int32_t type, int32_t act, const MoeProduct& p, int32_t ou
   };
   if (type == SPTIR_F16) with(_Float16{});
   else if (type == SPTIR_BF16) with(__bf16{});
-  else if constexpr (S::kBM == 128) with(float{});
+  else if constexpr (S::kBM <= 128) with(float{});
   SPTIR_HIP(hipGetLastError());
   return SPTIR_OK;
 }
@@ -565,24 +577,6 @@ sptir_status_t launch_best(int32_t type, int32_t act, bool words, const MoeProdu
 }
 
 }  // namespace
-
-double moe_tiles_forward_estimate(int32_t type, int32_t act, bool words, const MoeProduct& p) {
-  const int32_t out_cols = columns<kMoeForward>(act, p);
-  double us = estimate<kMoeForward, Narrow>(p, out_cols, columns<kMoeForward, Narrow>(act));
-  if (type == SPTIR_F32) us *= 6.5;
-  else if (!words) us *= 1.5;
-  else us = std::min(us, estimate<kMoeForward, Wide>(p, out_cols, columns<kMoeForward, Wide>(act)));
-  // ... and no less than the weights take from memory
-  return std::max(us, (double)std::min<int64_t>(p.n_rows, p.n_experts) * p.n_j * p.n_r * moe_type_bytes(type) / 4.1e6);
-}
-sptir_status_t moe_tiles_forward(int32_t type, int32_t act, bool words, const MoeProduct& p, hipStream_t stream) {
-  return launch_best<kMoeForward>(type, act, words, p, stream);
-}
-sptir_status_t moe_tiles_dx(int32_t type, int32_t act, bool words, const MoeProduct& p, hipStream_t stream) {
-  return launch_best<kMoeDx>(type, act, words, p, stream);
-}
-sptir_status_t moe_tiles_dw(int32_t type, bool words, const MoeProduct& p, hipStream_t stream) {
-  return launch_best<kMoeDw>(type, SPTIR_ACT_NONE, words, p, stream);
-}
-
 }  // namespace sptir
+
+#endif  // SPTIR_MOE_TILES_KERNEL_H_
