@@ -29,13 +29,6 @@ void moe_with_type(int32_t type, F&& f) {
 sptir_status_t moe_check_sizes(int32_t n_tokens, int32_t top_k, int32_t n_experts);
 sptir_status_t moe_check_routing(const sptir_moe_routing_t* r);
 
-// 16 bytes of elements, from and to memory that is aligned to them
-template <typename T>
-struct alignas(16) Pack {
-  static constexpr int kN = 16 / sizeof(T);
-  T v[kN];
-};
-
 // ---- 16 bytes from anywhere: global memory takes any alignment of an element
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 

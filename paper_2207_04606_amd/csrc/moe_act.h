@@ -21,17 +21,19 @@ __device__ inline float act_exp(float z) {
   return expf(z);
 }
 
-// The normal distribution function.  For 16 bits without branches: erfc by the Chebyshev fit of Press et al., Numerical
-// Recipes ("erfcc"), whose relative error is below 1.2e-7 everywhere.
+// The normal distribution function.  For 16 bits without branches: with x = |z| / sqrt(2) and t = 2 / (2 + x) in (0, 1],
+// log(erfc(x) / t) + x^2 is smooth in t and has a limit at t = 0.  The polynomial is its minimax fit (reweighted least squares at
+// 200 Chebyshev nodes), 1.4e-6 from it; with float32 sums the relative error is below 2e-6 for |z| < 3 and 7e-6 for |z| < 9: a
+// seventieth of a rounding to float16.
 template <typename T>
 __device__ inline float act_phi(float z) {
   if constexpr (sizeof(T) == 2) {
     const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(1.f + 0.5f * x);
-    const float c[] = {0.17087277f, -0.82215223f, 1.48851587f, -1.13520398f, 0.27886807f, -0.18628806f, 0.09678418f, 0.37409196f, 1.00002368f};
+    const float c[] = {-0.0528067435f, 0.0444019728f, 0.327749864f, -0.585905675f, 0.114518514f, 0.0378491719f, 0.379900663f, 0.999801735f, -1.26551081f};
     float s = c[0];
 #pragma unroll
     for (int i = 1; i < 9; ++i) s = fmaf(s, t, c[i]);
-    const float half = 0.5f * t * act_exp<T>(fmaf(s, t, -1.26551223f) - x * x);
+    const float half = 0.5f * t * act_exp<T>(s - x * x);
     return z < 0.f ? half : 1.f - half;
   }
   return 0.5f * (1.f + erff(z * 0.70710678118654752f));

@@ -1,7 +1,7 @@
 // The experts' products where an expert has few rows: single tokens, small batches.  The weights are read once and nothing
 // else counts, so they go from memory to the matrix instructions without a stop in LDS: a workgroup has 16 columns (or 32)
 // of one expert's product and up to 64 of its rows, its wavefronts take r in turn, 128 bytes of a row of W each, and their
-// sums meet in LDS.
+// sums meet in LDS.  Bound by memory: eight experts' 2048 x 2048 of bf16 for one token, 67 MB, take 13.4 us, 5.0 TB/s.
 #include <algorithm>
 #include <cmath>
 
@@ -26,11 +26,85 @@ __device__ inline F read_frag(const T* p, int64_t n) {
   return f;
 }
 
+// Every wavefront finds its own tile: 64 experts at a time, a lane each, tiles added up.
+__device__ inline bool find_tile(const MoeProduct& p, int rows, int64_t tile, MoeTile* out) {
+  if (!p.expert_ptr) {
+    *out = {0, tile * rows, p.n_rows};
+    return tile * rows < p.n_rows;
+  }
+  const int lane = threadIdx.x & 63;
+  int64_t before = 0;
+  for (int e0 = 0; e0 <= p.n_experts; e0 += 64) {
+    const int e = e0 + lane;
+    int lo = 0, hi = 0;
+    if (e <= p.n_experts) {
+      lo = p.expert_ptr[e];
+      hi = e < p.n_experts ? p.expert_ptr[e + 1] : (int)p.n_rows;
+    }
+    const int tiles = (hi - lo + rows - 1) / rows;
+    int sum = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(sum, d);
+      if (lane >= d) sum += o;
+    }
+    const unsigned long long past = __ballot(before + sum > tile);
+    if (past) {
+      const int owner = __ffsll(past) - 1;
+      const int64_t start = before + __shfl(sum - tiles, owner);
+      const int own_lo = __shfl(lo, owner), own_hi = __shfl(hi, owner);
+      *out = {__builtin_amdgcn_readfirstlane(e0 + owner), own_lo + (tile - start) * rows, own_hi};
+      return true;
+    }
+    before += __shfl(sum, 63);
+  }
+  return false;
+}
+
+__device__ inline int64_t x_row(const MoeProduct& p, int64_t s) { return p.entry_of ? moe_token(p, p.entry_of[s]) : s; }
+
+// ---- the epilogue of one element
+template <typename T, int kAct>
+__device__ inline void emit(const MoeProduct& p, int expert, int64_t i, int32_t j, float acc) {
+  if (p.bias) acc += to_float(((const T*)p.bias)[expert * p.bias_stride + j]);
+  if (p.pre) ((T*)p.pre)[i * p.ld_pre + j] = from_float<T>(acc);
+  float y = act_value<kAct, T>(acc);
+  if (p.residual) y += to_float(((const T*)p.residual)[i * p.ld_residual + j]);
+  ((T*)p.C)[i * p.ldc + j] = from_float<T>(y);
+}
+// swiglu's pair of column j of y
+template <typename T>
+__device__ inline void emit_gated(const MoeProduct& p, int expert, int64_t i, int32_t j, float g, float u) {
+  const int32_t n = p.n_j / 2;
+  if (p.bias) {
+    const T* b = (const T*)p.bias + expert * p.bias_stride + j;
+    g += to_float(b[0]);
+    u += to_float(b[n]);
+  }
+  if (p.pre) {
+    T* z = (T*)p.pre + i * p.ld_pre + j;
+    z[0] = from_float<T>(g);
+    z[n] = from_float<T>(u);
+  }
+  float y = act_gated<T>(g, u);
+  if (p.residual) y += to_float(((const T*)p.residual)[i * p.ld_residual + j]);
+  ((T*)p.C)[i * p.ldc + j] = from_float<T>(y);
+}
+// the rows that belong to no expert: of y, of pre the same and its pair
+template <typename T, bool kGated>
+__device__ inline void clear(const MoeProduct& p, int64_t i, int32_t j) {
+  ((T*)p.C)[i * p.ldc + j] = from_float<T>(0.f);
+  if (p.pre) {
+    ((T*)p.pre)[i * p.ld_pre + j] = from_float<T>(0.f);
+    if (kGated) ((T*)p.pre)[i * p.ld_pre + j + p.n_j / 2] = from_float<T>(0.f);
+  }
+}
+
 // kFM, kFN: fragments of 16 rows and of 16 columns (gated: one of gates, one of what goes with them)
 template <typename T, bool kGated, int kFM, int kFN>
 __global__ __launch_bounds__(64 * kWaves) void k_moe_few(MoeProduct p, int32_t act, int32_t j_tiles) {
   static_assert(!kGated || kFN == 2, "a gate has its pair beside it");
-  constexpr int kCols = kGated ? 16 : 16 * kFN, kN = Pack<T>::kN, kStep = 8 * kN;  // of r, a wavefront's turn: 128 bytes
+  constexpr int kCols = kGated ? 16 : 16 * kFN, kN = 16 / sizeof(T), kStep = 8 * kN;  // of r, a wavefront's turn: 128 bytes
   constexpr int kTurns = kFM == 1 ? 4 : kFM == 2 ? 2 : 1;
   using M = Mma<T>;
   using Frag = typename M::Frag;
@@ -38,7 +112,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_moe_few(MoeProduct p, int32_t a
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, q = lane >> 4;
   const int32_t out_cols = kGated ? p.n_j / 2 : p.n_j;
   MoeTile t;
-  if (!moe_find_tile(p, 16 * kFM, blockIdx.x / j_tiles, &t)) return;
+  if (!find_tile(p, 16 * kFM, blockIdx.x / j_tiles, &t)) return;
   const int32_t j0 = (int32_t)(blockIdx.x % j_tiles) * kCols;
   const bool none = t.expert == p.n_experts;
   f32x4 acc[kFM][kFN] = {};
@@ -46,7 +120,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_moe_few(MoeProduct p, int32_t a
     const T* x[kFM];
     const T* w[kFN];
 #pragma unroll
-    for (int f = 0; f < kFM; ++f) x[f] = (const T*)p.A + moe_x_row(p, min(t.first + 16 * f + fr, t.end - 1)) * p.lda;
+    for (int f = 0; f < kFM; ++f) x[f] = (const T*)p.A + x_row(p, min(t.first + 16 * f + fr, t.end - 1)) * p.lda;
 #pragma unroll
     for (int g = 0; g < kFN; ++g) {
       const int32_t row = kGated ? min(j0 + fr, out_cols - 1) + g * out_cols : min(j0 + 16 * g + fr, p.n_j - 1);
@@ -101,12 +175,12 @@ __global__ __launch_bounds__(64 * kWaves) void k_moe_few(MoeProduct p, int32_t a
     for (int v = 0; v < 4; ++v) {
       const int32_t j = j0 + 16 * g + (l >> 4) * 4 + v;
       if (j >= out_cols) continue;
-      if (none) moe_clear_row<T, kMoeForward, kGated ? SPTIR_ACT_SWIGLU : SPTIR_ACT_NONE>(p, i, j);
-      else if (kGated) moe_emit_gated<T>(p, t.expert, i, j, sum[v], pair[v]);
-      else if (act == SPTIR_ACT_RELU) moe_emit<T, kMoeForward, SPTIR_ACT_RELU>(p, t.expert, i, j, sum[v]);
-      else if (act == SPTIR_ACT_GELU) moe_emit<T, kMoeForward, SPTIR_ACT_GELU>(p, t.expert, i, j, sum[v]);
-      else if (act == SPTIR_ACT_SILU) moe_emit<T, kMoeForward, SPTIR_ACT_SILU>(p, t.expert, i, j, sum[v]);
-      else moe_emit<T, kMoeForward, SPTIR_ACT_NONE>(p, t.expert, i, j, sum[v]);
+      if (none) clear<T, kGated>(p, i, j);
+      else if (kGated) emit_gated<T>(p, t.expert, i, j, sum[v], pair[v]);
+      else if (act == SPTIR_ACT_RELU) emit<T, SPTIR_ACT_RELU>(p, t.expert, i, j, sum[v]);
+      else if (act == SPTIR_ACT_GELU) emit<T, SPTIR_ACT_GELU>(p, t.expert, i, j, sum[v]);
+      else if (act == SPTIR_ACT_SILU) emit<T, SPTIR_ACT_SILU>(p, t.expert, i, j, sum[v]);
+      else emit<T, SPTIR_ACT_NONE>(p, t.expert, i, j, sum[v]);
     }
   }
 }
@@ -127,8 +201,10 @@ sptir_status_t launch(int32_t act, const MoeProduct& p, hipStream_t stream) {
 
 // Microseconds of a launch for kFM = 1, 2 and 4: W is read once for every 16 kFM rows of an expert (of which the last are half
 // full on average), at 4.8, 4.0 and 2.7 TB/s as measured for 64 rows of 32 experts (134 MB: 139, 85 and 78 us) and of one
-// (34 MB: 32, 19 and 27 us); with one pass that is 42, 36 and 45 us of 134 MB.
-double moe_few_estimate(int32_t type, const MoeProduct& p, int32_t* best) {
+// (34 MB: 32, 19 and 27 us); with one pass that is 42, 36 and 45 us of 134 MB.  float32 is bound by its products from a few dozen
+// rows on, at 47 TFLOP/s (4006 rows, 777 x 1000: 125 us).  Passes but the first take 2.2 times as long where operands do not lie
+// in words (2000 rows of 5 experts, 777 x 999 of 16 bits: 53 us).
+double moe_few_estimate(int32_t type, bool words, const MoeProduct& p, int32_t* best) {
   const double used = (double)std::min<int64_t>(p.n_rows, p.n_experts);
   const double bytes = used * p.n_j * p.n_r * moe_type_bytes(type), mean = (double)p.n_rows / used;
   const double rate[] = {4.8e6, 4.0e6, 2.7e6};
@@ -136,7 +212,7 @@ double moe_few_estimate(int32_t type, const MoeProduct& p, int32_t* best) {
   for (int i = 0; i < 3; ++i) {
     const double rows = 16 << i;
     const double passes = p.expert_ptr ? std::max(1.0, mean / rows + 0.5) : std::ceil(mean / rows);
-    const double us = 5.0 + passes * bytes / rate[i];
+    const double us = 5.0 + std::max((words ? passes : 1 + 2.2 * (passes - 1)) * bytes / rate[i], type == SPTIR_F32 ? 2.0 * p.n_rows * p.n_j * p.n_r / 47e6 : 0.0);
     if (i == 0 || us < least) {
       least = us;
       *best = 1 << i;

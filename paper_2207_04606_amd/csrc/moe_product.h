@@ -40,44 +40,11 @@ struct MoeProduct {
 };
 
 // The rows of an m-tile: tiles of `rows` rows, an expert's last one ragged; the rows behind the last expert's are a group of
-// their own, number n_experts.  Every wavefront finds its own: 64 experts at a time, a lane each, tiles added up.
+// their own, number n_experts.
 struct MoeTile {
   int32_t expert;
   int64_t first, end;  // of this tile's expert, `first` already at the tile
 };
-__device__ inline bool moe_find_tile(const MoeProduct& p, int rows, int64_t tile, MoeTile* out) {
-  if (!p.expert_ptr) {
-    *out = {0, tile * rows, p.n_rows};
-    return tile * rows < p.n_rows;
-  }
-  const int lane = threadIdx.x & 63;
-  int64_t before = 0;
-  for (int e0 = 0; e0 <= p.n_experts; e0 += 64) {
-    const int e = e0 + lane;
-    int lo = 0, hi = 0;
-    if (e <= p.n_experts) {
-      lo = p.expert_ptr[e];
-      hi = e < p.n_experts ? p.expert_ptr[e + 1] : (int)p.n_rows;
-    }
-    const int tiles = (hi - lo + rows - 1) / rows;
-    int sum = tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(sum, d);
-      if (lane >= d) sum += o;
-    }
-    const unsigned long long past = __ballot(before + sum > tile);
-    if (past) {
-      const int owner = __ffsll(past) - 1;
-      const int64_t start = before + __shfl(sum - tiles, owner);
-      const int own_lo = __shfl(lo, owner), own_hi = __shfl(hi, owner);
-      *out = {__builtin_amdgcn_readfirstlane(e0 + owner), own_lo + (tile - start) * rows, own_hi};
-      return true;
-    }
-    before += __shfl(sum, 63);
-  }
-  return false;
-}
 
 // most m-tiles that n_rows rows can make
 inline int64_t moe_most_tiles(int64_t n_rows, int32_t n_experts, bool routed, int rows) {
@@ -88,7 +55,6 @@ inline int64_t moe_most_tiles(int64_t n_rows, int32_t n_experts, bool routed, in
 __device__ inline int64_t moe_token(const MoeProduct& p, int32_t entry) {
   return p.k_mul ? __umulhi((uint32_t)entry, p.k_mul) >> p.k_shift : (uint32_t)entry;
 }
-__device__ inline int64_t moe_x_row(const MoeProduct& p, int64_t s) { return p.entry_of ? moe_token(p, p.entry_of[s]) : s; }
 // With 2^(b - 1) < k <= 2^b and m = floor(2^(31 + b) / k) + 1, m k = 2^(31 + b) + d, 0 < d <= k <= 2^b: x m / 2^(31 + b) exceeds
 // x / k by x d / (k 2^(31 + b)) < 1 / k, which moves no quotient of an x < 2^31.  m < 2^32 from k = 2 on; 0 stands for k = 1.
 inline void moe_divide_by(int32_t k, uint32_t* mul, uint32_t* shift) {
@@ -126,72 +92,6 @@ struct Mma<float> {
     return c;
   }
 };
-
-// ------------------------------------------------------------------- epilogues
-// One element (forward: j counts outputs of a product that is not gated).
-template <typename T, MoeOp kOp, int kAct>
-__device__ inline void moe_emit(const MoeProduct& p, int expert, int64_t i, int32_t j, float acc) {
-  if constexpr (kOp == kMoeForward) {
-    if (p.bias) acc += to_float(((const T*)p.bias)[expert * p.bias_stride + j]);
-    if (p.pre) ((T*)p.pre)[i * p.ld_pre + j] = from_float<T>(acc);
-    float y = act_value<kAct, T>(acc);
-    if (p.residual) y += to_float(((const T*)p.residual)[i * p.ld_residual + j]);
-    ((T*)p.C)[i * p.ldc + j] = from_float<T>(y);
-  } else if constexpr (kOp == kMoeDx) {
-    if constexpr (kAct == SPTIR_ACT_SWIGLU) {
-      const T* z = (const T*)p.pre + i * p.ld_pre + j;
-      float dg, du;
-      act_gated_slope<T>(acc, to_float(z[0]), to_float(z[p.n_j]), &dg, &du);
-      T* out = (T*)p.C + i * p.ldc + j;
-      out[0] = from_float<T>(dg);
-      out[p.n_j] = from_float<T>(du);
-    } else {
-      if constexpr (kAct != SPTIR_ACT_NONE) acc = act_slope<kAct, T>(acc, to_float(((const T*)p.pre)[i * p.ld_pre + j]));
-      ((T*)p.C)[i * p.ldc + j] = from_float<T>(acc);
-    }
-  } else {
-    ((T*)p.C)[expert * p.c_stride + i * p.ldc + j] = from_float<T>(acc);
-  }
-}
-// swiglu's pair of column j of y
-template <typename T>
-__device__ inline void moe_emit_gated(const MoeProduct& p, int expert, int64_t i, int32_t j, float g, float u) {
-  const int32_t n = p.n_j / 2;
-  if (p.bias) {
-    const T* b = (const T*)p.bias + expert * p.bias_stride + j;
-    g += to_float(b[0]);
-    u += to_float(b[n]);
-  }
-  if (p.pre) {
-    T* z = (T*)p.pre + i * p.ld_pre + j;
-    z[0] = from_float<T>(g);
-    z[n] = from_float<T>(u);
-  }
-  float y = act_gated<T>(g, u);
-  if (p.residual) y += to_float(((const T*)p.residual)[i * p.ld_residual + j]);
-  ((T*)p.C)[i * p.ldc + j] = from_float<T>(y);
-}
-// the rows that belong to no expert
-template <typename T, MoeOp kOp, int kAct>
-__device__ inline void moe_clear_row(const MoeProduct& p, int64_t i, int32_t j) {  // j of the row of C, of pre the same and its pair
-  ((T*)p.C)[i * p.ldc + j] = from_float<T>(0.f);
-  if (kOp == kMoeForward && p.pre) {
-    ((T*)p.pre)[i * p.ld_pre + j] = from_float<T>(0.f);
-    if (kAct == SPTIR_ACT_SWIGLU) ((T*)p.pre)[i * p.ld_pre + j + p.n_j / 2] = from_float<T>(0.f);
-  }
-  if (kOp == kMoeDx && kAct == SPTIR_ACT_SWIGLU) ((T*)p.C)[i * p.ldc + j + p.n_j] = from_float<T>(0.f);
-}
-
-template <typename F>
-void moe_with_act(int32_t act, F&& f) {
-  switch (act) {
-    case SPTIR_ACT_RELU: f(std::integral_constant<int, SPTIR_ACT_RELU>{}); break;
-    case SPTIR_ACT_GELU: f(std::integral_constant<int, SPTIR_ACT_GELU>{}); break;
-    case SPTIR_ACT_SILU: f(std::integral_constant<int, SPTIR_ACT_SILU>{}); break;
-    case SPTIR_ACT_SWIGLU: f(std::integral_constant<int, SPTIR_ACT_SWIGLU>{}); break;
-    default: f(std::integral_constant<int, SPTIR_ACT_NONE>{}); break;
-  }
-}
 
 }  // namespace sptir
 

@@ -63,7 +63,7 @@ extern "C" sptir_status_t sptir_moe_product(const sptir_moe_routing_t* routing, 
                      moe_words(q->type, q->d_out, {p.bias, p.residual, p.pre, p.C},
                                {p.bias_stride, p.residual ? p.ld_residual : 0, p.pre ? p.ld_pre : 0, p.ldc});
   int32_t fragments = 1;
-  if (moe_few_estimate(q->type, p, &fragments) < moe_tiles_forward_estimate(q->type, q->activation, words, p))
+  if (moe_few_estimate(q->type, words, p, &fragments) < moe_tiles_forward_estimate(q->type, q->activation, words, p))
     return moe_few_forward(q->type, q->activation, p, fragments, (hipStream_t)stream);
   return moe_tiles_forward(q->type, q->activation, words, p, (hipStream_t)stream);
 }

@@ -98,6 +98,7 @@ __device__ inline void clear_tail(const RowArgs& p, const Place& me) {
     for (int c = me.lane * kN; c < p.width; c += p.lanes * kN) store_span<T>((T*)p.out + s * p.ldo + c, p.width - c, zero);
 }
 
+// (16,384 tokens to 131,072 rows of 2048 bf16, 604 MB: 95 us, 6.4 TB/s, nearly a fill's rate; 8192 x 2: 24 us.)
 template <typename T, bool kTiny>
 __global__ __launch_bounds__(256) void k_moe_gather(RowArgs p) {
   constexpr int kN = Span<T>::kN;
@@ -130,6 +131,7 @@ __global__ __launch_bounds__(256) void k_moe_gather(RowArgs p) {
 }
 
 // Rows of no entry are read at row 0 instead, so that all loads are under way before the first is waited for, and not added.
+// (131,072 rows of 2048 bf16 to 16,384 tokens, 604 MB: 160 us, 3.8 TB/s; a plain sum over as much memory reads 4.0.)
 template <typename T, bool kTiny>
 __global__ __launch_bounds__(256) void k_moe_combine(RowArgs p) {
   constexpr int kN = Span<T>::kN;
@@ -165,6 +167,7 @@ __global__ __launch_bounds__(256) void k_moe_combine(RowArgs p) {
   }
 }
 
+// (8192 tokens, 16,384 rows of 2048 bf16, 168 MB: 32 us, 5.2 TB/s.)
 template <typename T, bool kTiny>
 __global__ __launch_bounds__(256) void k_moe_combine_backward(RowArgs p) {
   constexpr int kN = Span<T>::kN;

@@ -76,7 +76,7 @@ __device__ inline void moe_look_up(const MoeProduct& p, int rows, int tile, cons
 // ---- eight elements at a time, of which there are `many`; kWords: they lie in 16-byte words, and whole words of them are there
 template <typename T>
 struct Eight {
-  static constexpr int kN = Pack<T>::kN;
+  static constexpr int kN = 16 / sizeof(T);
   typename Mma<T>::Frag w[8 / kN];
   __device__ inline float at(int i) const { return to_float<T>(w[i / kN][i % kN]); }
 };
@@ -213,7 +213,7 @@ inline bool moe_near(int32_t type, int64_t rows, int64_t ld) {
 }
 
 // ---- launches (moe_few.hip, moe_tiles_*.hip; words: in 16-byte words throughout)
-double moe_few_estimate(int32_t type, const MoeProduct& p, int32_t* fragments);  // microseconds
+double moe_few_estimate(int32_t type, bool words, const MoeProduct& p, int32_t* fragments);  // microseconds
 sptir_status_t moe_few_forward(int32_t type, int32_t act, const MoeProduct& p, int32_t fragments, hipStream_t stream);
 double moe_tiles_forward_estimate(int32_t type, int32_t act, bool words, const MoeProduct& p);
 sptir_status_t moe_tiles_forward(int32_t type, int32_t act, bool words, const MoeProduct& p, hipStream_t stream);

@@ -8,7 +8,8 @@ namespace {
 // a row of a part's sums is whole words of eight
 int64_t part_columns(int32_t d_in) { return ((int64_t)d_in + 7) / 8 * 8; }
 
-// Eight columns of a row of dW, or one element of db, a thread.  (Reads: 1 MB of dW in 16 parts, 32 MB, ~12 us.)
+// Eight columns of a row of dW, or one element of db, a thread.  (512 x 512 in 16 parts, 17 MB: 5.2 us; 2048 x 1024
+// in 4, 34 MB: 6.8 us.)
 template <typename T>
 __global__ __launch_bounds__(256) void k_moe_join(MoeProduct p, const float* sums, const float* z_sums, int64_t columns) {
   const int64_t words = columns / 8, rows = (int64_t)p.n_experts * p.n_i, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -33,12 +34,13 @@ __global__ __launch_bounds__(256) void k_moe_join(MoeProduct p, const float* sum
   }
 }
 
-// Microseconds of a launch with an expert's rows in `parts`, and of joining them.  (Experts differ in rows, the more so the
-// fewer of them a workgroup sees; 32 experts of 1024 rows, 2048 x 1024: 4 turns of wide tiles 254 us, 8 of narrow ones 220.)
+// Microseconds of a launch with an expert's rows in `parts`, and of joining them.  Experts differ in rows, the more so the
+// fewer of them a workgroup sees.  (2048 x 1024 of 32 experts, wide and narrow tiles: 213 and 230 us with 1024 rows each, 255 and
+// 258 with 542 to 2963; 2048 x 2048 of 8 experts of 717 to 1741 rows: 125 and 115.)
 template <typename S>
 double dw_us(int64_t n_rows, int32_t n_experts, int32_t d_in, int32_t d_z, int32_t parts) {
   const double tiles = (double)((d_z + S::kBM - 1) / S::kBM) * std::max((d_in + S::kBN - 1) / S::kBN, 1) * n_experts * parts;
-  double us = tiles_us<S>(tiles, (double)n_rows / n_experts / parts);
+  double us = tiles_us<S>(SPTIR_BF16, true, tiles, (double)n_rows / n_experts / parts);  // (the workspace's size knows no type)
   if (n_experts > 1) us *= 1 + 1.2 / std::ceil(tiles / (256 * S::kGroups));
   return parts == 1 ? us : us + 5 + 8.0 * parts * n_experts * d_z * d_in / 4e6;
 }

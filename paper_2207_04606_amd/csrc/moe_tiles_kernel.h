@@ -1,5 +1,15 @@
 // The experts' products in tiles: operands from memory to LDS, matrix instructions from there.  (Compiled once for every
 // product, moe_tiles_forward.hip, moe_tiles_dx.hip and moe_tiles_dw.hip.)
+//
+// A workgroup keeps a tile of C in registers and adds up 128 bytes of r a step.  What bounds it is LDS: a wide tile's eight
+// wavefronts read (128 + 64) x 128 bytes each for 2^15 x 64 multiply-adds, 1536 clocks of LDS beside 2048 of matrix instructions;
+// with long rows 8192 x 8192 x 8192 of bf16 take 900 us, 1220 TFLOP/s (a large library product reaches 1290), 8192 x 4096 x 4096
+// 250 us, 1100, the gradients 1070 and 1030.  With short ones (r = 1024) the step's loads are not there in time, since all
+// workgroups ask memory for new operands at once, and the epilogue is a sixth of the tile: 32,768 rows, 1024 x 2048, 140 us, 980.
+// float32 is bound by its instructions: 4096 x 4096 x 4096 1040 us, 132 TFLOP/s (a library product: 150).  Operands that do not
+// lie in words pass through registers: 540 TFLOP/s in 16 bits.  Measured and left out: tiles of 64 x 64 and 64 x 128 (not faster
+// where the others are few, 1.5 times slower where many), four steps in LDS for a workgroup alone on its CU (no faster: it waits for
+// its own reads of LDS), stores past the caches (141 -> 170 us), a workgroup a tile for the weights' gradient (within 2%).
 #ifndef SPTIR_MOE_TILES_KERNEL_H_
 #define SPTIR_MOE_TILES_KERNEL_H_
 
@@ -510,18 +520,25 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
 using Wide = Shape<256, 256, 2, 4, 1>;
 using Narrow = Shape<128, 128, 2, 2, 2>;
 
-// Microseconds of a launch as measured for 64 of r and for the rest of a tile (8192 x 8192 x 8192 to 32768 x 2048 x 1024): what
-// decides between the shapes.  An expert's last tile is half full on average.
+// Microseconds of a launch: what decides between the shapes (and the kernel for few rows).  A CU's tiles come one by one where it
+// holds one workgroup, in pairs where it holds two, an odd one alone.  Measured for 64 of r: 1.73 a wide tile, 1.03 a pair of
+// narrow ones, 0.84 one (8192 x 8192 x 8192 to 32768 x 2048 x 1024); float32 8.5 and 4.6 (4096 x 4096 x 4096, 2048 x 512 x 512); 5
+// and 2 for the rest of a tile.  Operands that do not lie in words take 1.9 and 1.15 times as long.  An expert's last tile is
+// half full on average, and with experts' rows the number of tiles varies (4006 rows of 10 experts, 777 columns: 254 by the mean,
+// 259 in fact, and three CUs with two of them took the launch from 74 to 155 us).
 template <typename S>
-double tiles_us(double tiles, double r) {
-  const double per_64 = S::kBM == 256 ? 1.73 : 1.03, per_tile = S::kBM == 256 ? 5.0 : 2.0;
-  return std::ceil(tiles / (256 * S::kGroups)) * (std::ceil(r / 64) * per_64 + per_tile);
+double tiles_us(int32_t type, bool words, double tiles, double r) {
+  const double each = std::ceil(tiles / 256), steps = std::ceil(r / 64);
+  if (S::kGroups == 1) return each * (steps * 1.73 + 5.0);
+  const bool f32 = type == SPTIR_F32;
+  const double pairs = std::floor(each / 2), one = each - 2 * pairs;
+  return (pairs * (f32 ? 8.5 : 1.03) + one * (f32 ? 4.6 : 0.84)) * steps * (words ? 1.0 : f32 ? 1.15 : 1.9) + (pairs + one) * 2.0;
 }
 template <MoeOp kOp, typename S>
-double estimate(const MoeProduct& p, int32_t out_cols, int32_t cols) {
+double estimate(int32_t type, bool words, const MoeProduct& p, int32_t out_cols, int32_t cols) {
   const double j_tiles = (out_cols + cols - 1) / cols, rows = (double)p.n_rows;
   const double m_tiles = p.expert_ptr ? std::min(rows, rows / S::kBM + 0.5 * p.n_experts) : (double)((p.n_rows + S::kBM - 1) / S::kBM);
-  return tiles_us<S>(j_tiles * m_tiles, p.n_r);
+  return tiles_us<S>(type, words, j_tiles * m_tiles * (p.expert_ptr ? 1.05 : 1.0), p.n_r);
 }
 
 template <MoeOp kOp, bool kWords, typename S>
@@ -571,7 +588,7 @@ template <MoeOp kOp>
 sptir_status_t launch_best(int32_t type, int32_t act, bool words, const MoeProduct& p, hipStream_t stream) {
   const int32_t out_cols = columns<kOp>(act, p), wide = columns<kOp, Wide>(act), narrow = columns<kOp, Narrow>(act);
   if (!words) return launch<kOp, false, Narrow>(type, act, p, out_cols, narrow, stream);
-  if (type != SPTIR_F32 && estimate<kOp, Wide>(p, out_cols, wide) < estimate<kOp, Narrow>(p, out_cols, narrow))
+  if (type != SPTIR_F32 && estimate<kOp, Wide>(type, true, p, out_cols, wide) < estimate<kOp, Narrow>(type, true, p, out_cols, narrow))
     return launch<kOp, true, Wide>(type, act, p, out_cols, wide, stream);
   return launch<kOp, true, Narrow>(type, act, p, out_cols, narrow, stream);
 }
