@@ -199,8 +199,8 @@ void with_lanes(int32_t n_experts, int32_t top_k, F&& f) {
 // wavefront counts its entries per expert in LDS, the counts become first places (experts ascending, inside an expert
 // parts ascending), and the wavefront then places its entries in order, 64 at a time: those of one expert are found with a
 // ballot per bit of the expert's number.  With more than one workgroup the counts of all of them come from a launch before.
-// Bound by latency: every step waits for the one before.  (131,072 entries, 128 experts: counts 3.3 us, places 9.8, of which the
-// sums of the workgroups' counts are the half; 8 entries in one launch: 3.9 us; the entries' 1.5 MB take 0.3.)
+// Bound by latency: every step waits for the one before.  (131,072 entries, 128 experts: counts 3.3 us, places 9.8; 8 entries, in one
+// launch: 3.9 us.  The 1.5 MB alone would take 0.3.)
 __device__ inline unsigned long long lanes_alike(int e, int bits) {
   unsigned long long m = ~0ull;
   for (int b = 0; b < bits; ++b) {

@@ -524,7 +524,7 @@ using Narrow = Shape<128, 128, 2, 2, 2>;
 // holds one workgroup, in pairs where it holds two, an odd one alone.  Measured for 64 of r: 1.73 a wide tile, 1.03 a pair of
 // narrow ones, 0.84 one (8192 x 8192 x 8192 to 32768 x 2048 x 1024); float32 8.5 and 4.6 (4096 x 4096 x 4096, 2048 x 512 x 512); 5
 // and 2 for the rest of a tile.  Operands that do not lie in words take 1.9 and 1.15 times as long.  An expert's last tile is
-// half full on average, and with experts' rows the number of tiles varies (4006 rows of 10 experts, 777 columns: 254 by the mean,
+// half full on average (one it has at least), and with experts' rows the number of tiles varies (4006 rows of 10 experts, 777 columns: 254 by the mean,
 // 259 in fact, and three CUs with two of them took the launch from 74 to 155 us).
 template <typename S>
 double tiles_us(int32_t type, bool words, double tiles, double r) {
@@ -537,7 +537,7 @@ double tiles_us(int32_t type, bool words, double tiles, double r) {
 template <MoeOp kOp, typename S>
 double estimate(int32_t type, bool words, const MoeProduct& p, int32_t out_cols, int32_t cols) {
   const double j_tiles = (out_cols + cols - 1) / cols, rows = (double)p.n_rows;
-  const double m_tiles = p.expert_ptr ? std::min(rows, rows / S::kBM + 0.5 * p.n_experts) : (double)((p.n_rows + S::kBM - 1) / S::kBM);
+  const double m_tiles = p.expert_ptr ? std::max(rows / S::kBM + 0.5 * p.n_experts, std::min(rows, (double)p.n_experts)) : (double)((p.n_rows + S::kBM - 1) / S::kBM);
   return tiles_us<S>(type, words, j_tiles * m_tiles * (p.expert_ptr ? 1.05 : 1.0), p.n_r);
 }
 
