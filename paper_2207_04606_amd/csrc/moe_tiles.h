@@ -73,6 +73,29 @@ __device__ inline void moe_look_up(const MoeProduct& p, int rows, int tile, cons
           __builtin_amdgcn_readfirstlane(table.row[e + 1])};
 }
 
+// (dw) The experts from the one with the most rows to the one with the fewest, in LDS: what a workgroup adds up then differs
+// less, and the long tiles do not come last.  (For as many as take a microsecond to rank; more of them even out.  32 experts with
+// 542 to 2963 rows, 2048 x 1024: 255 -> 234 us; with 1024 rows each 1 us more.)
+constexpr int kMoeRanked = 128;
+inline __host__ __device__ bool moe_ranks(const MoeProduct& p) { return p.expert_ptr && p.n_experts > 1 && p.n_experts <= kMoeRanked; }
+inline int moe_ranks_bytes(const MoeProduct& p) { return moe_ranks(p) ? 2 * p.n_experts * (int)sizeof(int32_t) : 0; }
+__device__ inline const int32_t* moe_rank_experts(const MoeProduct& p, int32_t* rows) {
+  if (!moe_ranks(p)) return nullptr;
+  int32_t* order = rows + p.n_experts;
+  const int e = threadIdx.x;  // (a thread each)
+  if (e < p.n_experts) rows[e] = p.expert_ptr[e + 1] - p.expert_ptr[e];
+  __syncthreads();
+  if (e < p.n_experts) {
+    const int mine = rows[e];
+    int rank = 0;
+#pragma unroll 8
+    for (int o = 0; o < p.n_experts; ++o) rank += rows[o] > mine || (rows[o] == mine && o < e);
+    order[rank] = e;
+  }
+  __syncthreads();
+  return order;
+}
+
 // ---- eight elements at a time, of which there are `many`; kWords: they lie in 16-byte words, and whole words of them are there
 template <typename T>
 struct Eight {

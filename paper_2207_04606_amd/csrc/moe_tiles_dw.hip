@@ -35,8 +35,8 @@ __global__ __launch_bounds__(256) void k_moe_join(MoeProduct p, const float* sum
 }
 
 // Microseconds of a launch with an expert's rows in `parts`, and of joining them.  Experts differ in rows, the more so the
-// fewer of them a workgroup sees.  (2048 x 1024 of 32 experts, wide and narrow tiles: 213 and 230 us with 1024 rows each, 255 and
-// 258 with 542 to 2963; 2048 x 2048 of 8 experts of 717 to 1741 rows: 125 and 115.)
+// fewer of them a workgroup sees.  (Measured before they were ranked, wide and narrow tiles: 2048 x 1024 of 32 experts 213 and
+// 230 us with 1024 rows each, 255 and 258 with 542 to 2963; 2048 x 2048 of 8 experts of 717 to 1741 rows 125 and 115.)
 template <typename S>
 double dw_us(int64_t n_rows, int32_t n_experts, int32_t d_in, int32_t d_z, int32_t parts) {
   const double tiles = (double)((d_z + S::kBM - 1) / S::kBM) * std::max((d_in + S::kBN - 1) / S::kBN, 1) * n_experts * parts;

@@ -41,7 +41,7 @@ struct Shape {
   static constexpr int kFM = kBM / kWavesM / 16, kFN = kBN / kWavesN / 16;  // fragments of a wavefront's tile
   static_assert(kFN == 4, "a wavefront has 64 columns");
   static constexpr int kBytesA = kBM * 128, kBytesB = kBN * 128, kStage = kBytesA + kBytesB;
-  static_assert(kGroups * (2 * kStage + 2 * 1024) <= 160 * 1024, "LDS, with the table of 250 experts");
+  static_assert(kThreads >= kMoeRanked && kGroups * (2 * kStage + 2 * 1024) <= 160 * 1024, "LDS, with the table of 250 experts");
 };
 
 // Which 16-byte chunk of a line lies at place `pos` of it in LDS: pos ^ key(line), so that the lanes that read together find
@@ -113,6 +113,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   // ---- the tiles of this workgroup
   const uint32_t per_expert = (uint32_t)i_tiles * j_tiles;
   const MoeTable table = {(int32_t*)(lds_generic + 2 * S::kStage), (int32_t*)(lds_generic + 2 * S::kStage) + p.n_experts + 2};
+  const int32_t* order = kOp == kMoeDw ? moe_rank_experts(p, (int32_t*)(lds_generic + 2 * S::kStage)) : nullptr;
   const uint32_t m_tiles = kOp == kMoeDw ? 0 : moe_fill_table(p, S::kBM, table);
   const uint32_t total = kOp == kMoeDw ? per_expert * p.n_experts * (kEnd >= kEndParts ? p.parts : 1) : m_tiles * j_tiles;
   MoeTile t;
@@ -145,11 +146,19 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   constexpr bool kSumZ = kOp == kMoeDw && (kEnd == kEndAct || kEnd == kEndPartsSum);  // (db is asked for)
   bool sum_z = false;  // this tile's workgroup sums dZ too
   auto start = [&](uint32_t id) __attribute__((always_inline)) {
-    const uint32_t dealt = moe_deal(id, total);
+    uint32_t dealt = moe_deal(id, total);
     int jt;
     if constexpr (kOp == kMoeDw) {
-      const int which = (int)(dealt / per_expert), e = kParts ? which % p.n_experts : which;
-      int it;
+      if (order && id / gridDim.x % 2) {  // (every other turn the other way round: a workgroup with a long one has a short one next)
+        const uint32_t first = id - blockIdx.x;
+        dealt = first + min(first + gridDim.x, total) - 1 - dealt;
+      }
+      int which = (int)(dealt / per_expert), e = kParts ? which % p.n_experts : which, it;
+      if (order) {
+        const int ranked = __builtin_amdgcn_readfirstlane(order[e]);
+        which += ranked - e;
+        e = ranked;
+      }
       moe_square(dealt % per_expert, i_tiles, j_tiles, &it, &jt);
       t = {which, (int64_t)it * S::kBM, p.n_i};
       r0 = p.expert_ptr ? p.expert_ptr[e] : 0;
@@ -552,7 +561,7 @@ sptir_status_t launch(int32_t type, int32_t act, const MoeProduct& p, int32_t ou
   auto go = [&](auto v, auto end) {
     auto* kernel = k_moe_tiles<decltype(v), kOp, decltype(end)::value, kWords, S>;
     static OncePerDevice allowed;
-    const int lds = 2 * S::kStage + (kOp == kMoeDw ? 0 : moe_table_bytes(p.expert_ptr, p.n_experts));
+    const int lds = 2 * S::kStage + (kOp == kMoeDw ? moe_ranks_bytes(p) : moe_table_bytes(p.expert_ptr, p.n_experts));
     allow_dynamic_lds((const void*)kernel, lds, allowed);
     hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(S::kThreads), lds, stream, p, act, (int32_t)j_tiles, (int32_t)i_tiles);
   };
