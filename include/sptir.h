@@ -621,7 +621,8 @@ sptir_status_t sptir_moe_product_dx(const sptir_moe_routing_t* routing, const sp
 
 /*
  * dW[e] = sum over the rows s of expert e of dZ[s] x^T and db[e] = sum of dZ[s] (db may be NULL); zeros for an expert
- * without rows.  `workspace`: sptir_moe_product_dw_workspace bytes (0: may be NULL), free again once the work is done.
+ * without rows.  `workspace`: sptir_moe_product_dw_workspace bytes (0: may be NULL) at a multiple of 16, free again once the
+ * work is done: where dW is small and rows are many, they are summed in parts, which are added up in their order.
  */
 typedef struct {
   int32_t struct_size;
