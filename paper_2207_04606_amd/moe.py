@@ -5,6 +5,7 @@ int32.  A matrix may have any row stride, its rows have to be contiguous.  Outpu
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 
 import torch
@@ -14,6 +15,7 @@ from .binding import SPTIR_OK, SptirError, _dev, _stream_ptr, load_library
 TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "swiglu": 4}
 _NULL = (None, 0)
+_NOTHING = contextlib.nullcontext()
 
 
 class _Routing(ctypes.Structure):
@@ -118,14 +120,23 @@ def _per_entry(t, dtype, shape, what):
     return t.data_ptr() or None
 
 
+def _under(stream):
+    """The context in which memory for a call on `stream` is allocated.  The caching allocator orders a block's reuse against the
+    stream it is taken under only: one taken under the current stream may still be in use there when the call's kernels begin."""
+    if stream is None:
+        return _NOTHING
+    if not isinstance(stream, torch.cuda.Stream):
+        number = int(getattr(stream, "cuda_stream", stream))
+        stream = torch.cuda.ExternalStream(number) if number else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
+
+
 def _workspace(nbytes, stream):
-    """Device memory for one call; the caching allocator must not give it to others before `stream` is done with it."""
+    """Device memory for one call."""
     if nbytes == 0:
         return None
-    t = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
-    if stream is not None:
-        t.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
-    return t
+    with _under(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
 
 
 class MoeRouting:
@@ -188,10 +199,11 @@ def sptir_moe_sort(experts, n_experts: int, routing: MoeRouting | None = None, s
     T, k = experts.shape
     n = T * k
     if routing is None:
-        new = [torch.empty(m, dtype=torch.int32, device=experts.device) for m in (max(int(n_experts), 0) + 1, n, n)]
-        if stream is not None:
+        with _under(stream):
+            new = [torch.empty(m, dtype=torch.int32, device=experts.device) for m in (max(int(n_experts), 0) + 1, n, n)]
+        if stream is not None:  # (the caller will use them under the current stream)
             for t in new:
-                t.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
+                t.record_stream(torch.cuda.current_stream())
         routing = MoeRouting(T, k, int(n_experts), *new)
     elif (routing.n_tokens, routing.top_k, routing.n_experts) != (T, k, n_experts):
         raise ValueError("routing has arrays of other sizes")
