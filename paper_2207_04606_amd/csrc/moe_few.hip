@@ -3,7 +3,6 @@
 // of one expert's product and up to 64 of its rows, its wavefronts take r in turn, 128 bytes of a row of W each, and their
 // sums meet in LDS.  Bound by memory: eight experts' 2048 x 2048 of bf16 for one token, 67 MB, take 13.4 us, 5.0 TB/s.
 #include <algorithm>
-#include <cmath>
 
 #include "moe_tiles.h"
 
@@ -198,30 +197,6 @@ sptir_status_t launch(int32_t act, const MoeProduct& p, hipStream_t stream) {
 }
 
 }  // namespace
-
-// Microseconds of a launch for kFM = 1, 2 and 4: W is read once for every 16 kFM rows of an expert (of which the last are half
-// full on average), at 4.8, 4.0 and 2.7 TB/s as measured for 64 rows of 32 experts (134 MB: 139, 85 and 78 us) and of one
-// (34 MB: 32, 19 and 27 us); with one pass that is 42, 36 and 45 us of 134 MB.  float32 is bound by its products from a few dozen
-// rows on, at 47 TFLOP/s (4006 rows, 777 x 1000: 125 us).  Passes but the first take 2.2 times as long where operands do not lie
-// in words (2000 rows of 5 experts, 777 x 999 of 16 bits: 53 us).  Both sides, this kernel's and the tiles': 32 experts of
-// 2048 x 1024 with 1, 4, 12 and 64 rows each 18 and 20, 28 and 23, 32 and 24, 73 and 62 us; 64 of 2048 x 2048 with 1 row 60 and 73,
-// with 8 128 and 125; one of 4096 x 4096 with 16, 128 and 256 rows 10 and 42, 26 and 44, 47 and 44.
-double moe_few_estimate(int32_t type, bool words, const MoeProduct& p, int32_t* best) {
-  const double used = (double)std::min<int64_t>(p.n_rows, p.n_experts);
-  const double bytes = used * p.n_j * p.n_r * moe_type_bytes(type), mean = (double)p.n_rows / used;
-  const double rate[] = {4.8e6, 4.0e6, 2.7e6};
-  double least = 0;
-  for (int i = 0; i < 3; ++i) {
-    const double rows = 16 << i;
-    const double full = mean / rows, passes = p.expert_ptr ? 1 + full * full / (full + 0.5) : std::ceil(full);  // (towards full + 0.5)
-    const double us = 5.0 + std::max((words ? passes : 1 + 2.2 * (passes - 1)) * bytes / rate[i], type == SPTIR_F32 ? 2.0 * p.n_rows * p.n_j * p.n_r / 47e6 : 0.0);
-    if (i == 0 || us < least) {
-      least = us;
-      *best = 1 << i;
-    }
-  }
-  return least;
-}
 
 sptir_status_t moe_few_forward(int32_t type, int32_t act, const MoeProduct& p, int32_t fragments, hipStream_t stream) {
   sptir_status_t st = SPTIR_OK;

@@ -6,6 +6,7 @@
 
 #include "moe.h"
 #include "moe_act.h"
+#include "moe_choice.h"
 
 namespace sptir {
 
@@ -45,12 +46,6 @@ struct MoeTile {
   int32_t expert;
   int64_t first, end;  // of this tile's expert, `first` already at the tile
 };
-
-// most m-tiles that n_rows rows can make
-inline int64_t moe_most_tiles(int64_t n_rows, int32_t n_experts, bool routed, int rows) {
-  if (!routed) return (n_rows + rows - 1) / rows;
-  return std::min<int64_t>(n_rows, n_rows / rows + n_experts + 1);
-}
 
 __device__ inline int64_t moe_token(const MoeProduct& p, int32_t entry) {
   return p.k_mul ? __umulhi((uint32_t)entry, p.k_mul) >> p.k_shift : (uint32_t)entry;

@@ -23,6 +23,10 @@ sptir_status_t take_routing(const sptir_moe_routing_t* routing, int64_t n_rows, 
   return SPTIR_OK;
 }
 
+MoeSizes sizes_of(int32_t type, bool words, bool gated, const MoeProduct& p) {
+  return {p.n_rows, p.n_experts, p.expert_ptr != nullptr, p.n_j, p.n_r, type == SPTIR_F32, words, gated};
+}
+
 bool act_ok(int32_t act) { return act >= SPTIR_ACT_NONE && act <= SPTIR_ACT_SWIGLU; }
 // Weights that are read may be shared by experts (stride 0); where they are written, neither rows nor matrices overlap.
 bool weights_ok(int64_t ld, int64_t stride, int64_t cols) { return ld >= cols && stride >= 0; }
@@ -62,10 +66,9 @@ extern "C" sptir_status_t sptir_moe_product(const sptir_moe_routing_t* routing, 
                      moe_words(q->type, q->d_in, {p.A, p.B}, {p.lda, p.ldb, p.b_stride}) &&
                      moe_words(q->type, q->d_out, {p.bias, p.residual, p.pre, p.C},
                                {p.bias_stride, p.residual ? p.ld_residual : 0, p.pre ? p.ld_pre : 0, p.ldc});
-  int32_t fragments = 1;
-  if (moe_few_estimate(q->type, words, p, &fragments) < moe_tiles_forward_estimate(q->type, q->activation, words, p))
-    return moe_few_forward(q->type, q->activation, p, fragments, (hipStream_t)stream);
-  return moe_tiles_forward(q->type, q->activation, words, p, (hipStream_t)stream);
+  const MoeChoice c = moe_choose_forward(sizes_of(q->type, words, q->activation == SPTIR_ACT_SWIGLU, p));
+  if (c.few) return moe_few_forward(q->type, q->activation, p, c.fragments, (hipStream_t)stream);
+  return moe_tiles_forward(q->type, q->activation, words, c.wide, p, (hipStream_t)stream);
 }
 
 extern "C" sptir_status_t sptir_moe_product_dx(const sptir_moe_routing_t* routing, const sptir_moe_product_dx_t* q, void* stream) {
@@ -89,12 +92,13 @@ extern "C" sptir_status_t sptir_moe_product_dx(const sptir_moe_routing_t* routin
   p.C = q->dX; p.ldc = q->ld_dx;
   const bool words = moe_near(q->type, p.n_rows, p.lda) && moe_near(q->type, kMoeStep, p.ldb) && moe_words(q->type, q->d_z, {p.A}, {p.lda}) &&
                      moe_words(q->type, q->d_in, {p.B, act ? p.pre : nullptr, p.C}, {p.ldb, p.b_stride, act ? p.ld_pre : 0, p.ldc});
-  return moe_tiles_dx(q->type, q->activation, words, p, (hipStream_t)stream);
+  const MoeChoice c = moe_choose_dx(sizes_of(q->type, words, false, p));
+  return moe_tiles_dx(q->type, q->activation, words, c.wide, p, (hipStream_t)stream);
 }
 
 extern "C" int64_t sptir_moe_product_dw_workspace(int64_t n_rows, int32_t n_experts, int32_t d_in, int32_t d_z) {
   if (n_rows <= 0 || n_experts <= 0 || d_in < 0 || d_z <= 0) return 0;
-  return moe_tiles_dw_workspace(moe_tiles_dw_parts(n_rows, n_experts, d_in, d_z), n_experts, d_in, d_z);
+  return moe_dw_workspace(moe_dw_parts(n_rows, n_experts, d_in, d_z), n_experts, d_in, d_z);
 }
 
 extern "C" sptir_status_t sptir_moe_product_dw(const sptir_moe_routing_t* routing, const sptir_moe_product_dw_t* q, void* stream) {

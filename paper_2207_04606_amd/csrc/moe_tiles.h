@@ -236,13 +236,9 @@ inline bool moe_near(int32_t type, int64_t rows, int64_t ld) {
 }
 
 // ---- launches (moe_few.hip, moe_tiles_*.hip; words: in 16-byte words throughout)
-double moe_few_estimate(int32_t type, bool words, const MoeProduct& p, int32_t* fragments);  // microseconds
 sptir_status_t moe_few_forward(int32_t type, int32_t act, const MoeProduct& p, int32_t fragments, hipStream_t stream);
-double moe_tiles_forward_estimate(int32_t type, int32_t act, bool words, const MoeProduct& p);
-sptir_status_t moe_tiles_forward(int32_t type, int32_t act, bool words, const MoeProduct& p, hipStream_t stream);
-sptir_status_t moe_tiles_dx(int32_t type, int32_t act, bool words, const MoeProduct& p, hipStream_t stream);
-int32_t moe_tiles_dw_parts(int64_t n_rows, int32_t n_experts, int32_t d_in, int32_t d_z);  // (of an expert's rows)
-int64_t moe_tiles_dw_workspace(int32_t parts, int32_t n_experts, int32_t d_in, int32_t d_z);
+sptir_status_t moe_tiles_forward(int32_t type, int32_t act, bool words, bool wide, const MoeProduct& p, hipStream_t stream);
+sptir_status_t moe_tiles_dx(int32_t type, int32_t act, bool words, bool wide, const MoeProduct& p, hipStream_t stream);
 sptir_status_t moe_tiles_dw(int32_t type, bool words, const MoeProduct& p, void* workspace, hipStream_t stream);
 
 }  // namespace sptir

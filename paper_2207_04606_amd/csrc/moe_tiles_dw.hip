@@ -5,9 +5,6 @@
 namespace sptir {
 namespace {
 
-// a row of a part's sums is whole words of eight
-int64_t part_columns(int32_t d_in) { return ((int64_t)d_in + 7) / 8 * 8; }
-
 // Eight columns of a row of dW, or one element of db, a thread.  (512 x 512 in 16 parts, 17 MB: 5.2 us; 2048 x 1024
 // in 4, 34 MB: 6.8 us.)
 template <typename T>
@@ -34,43 +31,16 @@ __global__ __launch_bounds__(256) void k_moe_join(MoeProduct p, const float* sum
   }
 }
 
-// Microseconds of a launch with an expert's rows in `parts`, and of joining them.  Experts differ in rows, the more so the
-// fewer of them a workgroup sees.  (Measured before they were ranked, wide and narrow tiles: 2048 x 1024 of 32 experts 213 and
-// 230 us with 1024 rows each, 255 and 258 with 542 to 2963; 2048 x 2048 of 8 experts of 717 to 1741 rows 125 and 115.)
-template <typename S>
-double dw_us(int64_t n_rows, int32_t n_experts, int32_t d_in, int32_t d_z, int32_t parts) {
-  const double tiles = (double)((d_z + S::kBM - 1) / S::kBM) * std::max((d_in + S::kBN - 1) / S::kBN, 1) * n_experts * parts;
-  double us = tiles_us<S>(SPTIR_BF16, true, tiles, (double)n_rows / n_experts / parts);  // (the workspace's size knows no type)
-  if (n_experts > 1) us *= 1 + 1.2 / std::ceil(tiles / (256 * S::kGroups));
-  return parts == 1 ? us : us + 5 + 8.0 * parts * n_experts * d_z * d_in / 4e6;
-}
-
 }  // namespace
-
-int32_t moe_tiles_dw_parts(int64_t n_rows, int32_t n_experts, int32_t d_in, int32_t d_z) {
-  int32_t best = 1;
-  double least = dw_us<Narrow>(n_rows, n_experts, d_in, d_z, 1);
-  for (int32_t parts = 2; parts <= 64 && n_rows / n_experts / parts >= 64; ++parts) {
-    const double us = dw_us<Narrow>(n_rows, n_experts, d_in, d_z, parts);
-    if (us < 0.9 * least) {
-      least = us;
-      best = parts;
-    }
-  }
-  return best;
-}
-int64_t moe_tiles_dw_workspace(int32_t parts, int32_t n_experts, int32_t d_in, int32_t d_z) {
-  return parts == 1 ? 0 : (int64_t)sizeof(float) * parts * n_experts * d_z * (part_columns(d_in) + 1);
-}
 
 sptir_status_t moe_tiles_dw(int32_t type, bool words, const MoeProduct& given, void* workspace, hipStream_t stream) {
   MoeProduct p = given;
-  p.parts = moe_tiles_dw_parts(p.n_rows, p.n_experts, p.n_j, p.n_i);
-  if (words && type != SPTIR_F32 && dw_us<Wide>(p.n_rows, p.n_experts, p.n_j, p.n_i, 1) < dw_us<Narrow>(p.n_rows, p.n_experts, p.n_j, p.n_i, p.parts)) {
+  p.parts = moe_dw_parts(p.n_rows, p.n_experts, p.n_j, p.n_i);
+  if (moe_dw_wide_pays(p.n_rows, p.n_experts, p.n_j, p.n_i, p.parts, type == SPTIR_F32, words)) {
     p.parts = 1;
     return launch<kMoeDw, true, Wide>(type, SPTIR_ACT_NONE, p, p.n_j, Wide::kBN, stream);
   }
-  const int64_t columns = part_columns(p.n_j), rows = (int64_t)p.n_experts * p.n_i;
+  const int64_t columns = moe_part_columns(p.n_j), rows = (int64_t)p.n_experts * p.n_i;
   if (p.parts > 1) {
     p.C = workspace;
     p.ldc = columns;

@@ -3,8 +3,8 @@
 
 namespace sptir {
 
-sptir_status_t moe_tiles_dx(int32_t type, int32_t act, bool words, const MoeProduct& p, hipStream_t stream) {
-  return launch_best<kMoeDx>(type, act, words, p, stream);
+sptir_status_t moe_tiles_dx(int32_t type, int32_t act, bool words, bool wide, const MoeProduct& p, hipStream_t stream) {
+  return launch_tiles<kMoeDx>(type, act, words, wide, p, stream);
 }
 
 }  // namespace sptir

@@ -14,7 +14,6 @@
 #define SPTIR_MOE_TILES_KERNEL_H_
 
 #include <algorithm>
-#include <cmath>
 #include <utility>
 
 #include "moe_tiles.h"
@@ -524,31 +523,9 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   }
 }
 
-// Two shapes of tiles.  Wide ones read LDS least for a matrix instruction, but come in few and one workgroup fills a CU; of
-// the others a CU holds two workgroups, and what is over at the ends of rows, experts and turns is a quarter.
-using Wide = Shape<256, 256, 2, 4, 1>;
-using Narrow = Shape<128, 128, 2, 2, 2>;
-
-// Microseconds of a launch: what decides between the shapes (and the kernel for few rows).  A CU's tiles come one by one where it
-// holds one workgroup, in pairs where it holds two, an odd one alone.  Measured for 64 of r: 1.73 a wide tile, 1.03 a pair of
-// narrow ones, 0.84 one (8192 x 8192 x 8192 to 32768 x 2048 x 1024); float32 8.5 and 4.6 (4096 x 4096 x 4096, 2048 x 512 x 512); 5
-// and 2 for the rest of a tile.  Operands that do not lie in words take 1.9 and 1.15 times as long.  An expert's last tile is
-// half full on average (one it has at least), and with experts' rows the number of tiles varies (4006 rows of 10 experts, 777 columns: 254 by the mean,
-// 259 in fact, and three CUs with two of them took the launch from 74 to 155 us).
-template <typename S>
-double tiles_us(int32_t type, bool words, double tiles, double r) {
-  const double each = std::ceil(tiles / 256), steps = std::ceil(r / 64);
-  if (S::kGroups == 1) return each * (steps * 1.73 + 5.0);
-  const bool f32 = type == SPTIR_F32;
-  const double pairs = std::floor(each / 2), one = each - 2 * pairs;
-  return (pairs * (f32 ? 8.5 : 1.03) + one * (f32 ? 4.6 : 0.84)) * steps * (words ? 1.0 : f32 ? 1.15 : 1.9) + (pairs + one) * 2.0;
-}
-template <MoeOp kOp, typename S>
-double estimate(int32_t type, bool words, const MoeProduct& p, int32_t out_cols, int32_t cols) {
-  const double j_tiles = (out_cols + cols - 1) / cols, rows = (double)p.n_rows;
-  const double m_tiles = p.expert_ptr ? std::max(rows / S::kBM + 0.5 * p.n_experts, std::min(rows, (double)p.n_experts)) : (double)((p.n_rows + S::kBM - 1) / S::kBM);
-  return tiles_us<S>(type, words, j_tiles * m_tiles * (p.expert_ptr ? 1.05 : 1.0), p.n_r);
-}
+// (moe_choice.h: when which)
+using Wide = Shape<kMoeWide.rows, kMoeWide.cols, 2, 4, kMoeWide.groups>;
+using Narrow = Shape<kMoeNarrow.rows, kMoeNarrow.cols, 2, 2, kMoeNarrow.groups>;
 
 template <MoeOp kOp, bool kWords, typename S>
 sptir_status_t launch(int32_t type, int32_t act, const MoeProduct& p, int32_t out_cols, int32_t cols, hipStream_t stream) {
@@ -594,12 +571,11 @@ template <MoeOp kOp>
 int32_t columns(int32_t act, const MoeProduct& p) { return kOp == kMoeForward && act == SPTIR_ACT_SWIGLU ? p.n_j / 2 : p.n_j; }
 
 template <MoeOp kOp>
-sptir_status_t launch_best(int32_t type, int32_t act, bool words, const MoeProduct& p, hipStream_t stream) {
-  const int32_t out_cols = columns<kOp>(act, p), wide = columns<kOp, Wide>(act), narrow = columns<kOp, Narrow>(act);
-  if (!words) return launch<kOp, false, Narrow>(type, act, p, out_cols, narrow, stream);
-  if (type != SPTIR_F32 && estimate<kOp, Wide>(type, true, p, out_cols, wide) < estimate<kOp, Narrow>(type, true, p, out_cols, narrow))
-    return launch<kOp, true, Wide>(type, act, p, out_cols, wide, stream);
-  return launch<kOp, true, Narrow>(type, act, p, out_cols, narrow, stream);
+sptir_status_t launch_tiles(int32_t type, int32_t act, bool words, bool wide, const MoeProduct& p, hipStream_t stream) {
+  const int32_t out_cols = columns<kOp>(act, p);
+  if (!words) return launch<kOp, false, Narrow>(type, act, p, out_cols, columns<kOp, Narrow>(act), stream);
+  if (wide) return launch<kOp, true, Wide>(type, act, p, out_cols, columns<kOp, Wide>(act), stream);
+  return launch<kOp, true, Narrow>(type, act, p, out_cols, columns<kOp, Narrow>(act), stream);
 }
 
 }  // namespace

@@ -1,0 +1,62 @@
+"""Which kernel takes a product of an expert layer (csrc/moe_choice.h, compiled alone): the sizes of test_gpu_moe_wide.py take more large
+tiles than the card has CUs, and every kernel takes some."""
+import os
+import subprocess
+
+import pytest
+
+import moe_wide_shapes as wide
+from paper_2207_04606_amd import build as sptir_build
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+
+@pytest.fixture(scope="module")
+def choice(tmp_path_factory):
+    exe = str(tmp_path_factory.mktemp("choice") / "choice")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-Wno-unused-function", "-I", sptir_build.CSRC,
+                           "-o", exe, os.path.join(HERE, "moe_choice_main.cpp")])
+
+    def ask(op, *sizes):  # (few, wide, fragments, parts)
+        out = subprocess.run([exe], input=" ".join(str(int(v)) if v is not op else v for v in (op, *sizes)), check=True, capture_output=True, text=True)
+        return tuple(int(v) for v in out.stdout.split())
+
+    return ask
+
+
+@pytest.mark.parametrize("T,k,E,d_in,d_out,act,dropped", wide.FORWARD)
+def test_large_tiles_of_the_product(choice, T, k, E, d_in, d_out, act, dropped):
+    few, is_wide, _, _ = choice("forward", T * k, max(E, 1), E > 0, wide.columns(d_out, act), d_in, 0, 1, act == "swiglu")
+    assert not few and is_wide
+    assert wide.tiles(T * k * (1 - dropped), wide.columns(d_out, act)) > 256
+
+
+@pytest.mark.parametrize("T,k,E,d_in,d_out,act,dropped", wide.DX)
+def test_large_tiles_of_the_inputs_gradient(choice, T, k, E, d_in, d_out, act, dropped):
+    assert choice("dx", T * k, max(E, 1), E > 0, d_in, d_out, 0, 1, 0)[:2] == (0, 1)
+    assert wide.tiles(T * k * (1 - dropped), d_in) > 256
+
+
+@pytest.mark.parametrize("T,k,E,d_in,d_out,dropped", wide.DW)
+def test_large_tiles_of_the_weights_gradient(choice, T, k, E, d_in, d_out, dropped):
+    assert choice("dw", T * k, max(E, 1), d_in, d_out, 0, 1) == (0, 1, 1, 1)
+    assert max(E, 1) * wide.tiles(d_out, d_in) > 256
+
+
+def test_no_large_tiles_of_float32_or_odd_operands(choice):
+    for f32, words in ((1, 1), (0, 0), (1, 0)):
+        assert choice("forward", 8192, 1, 0, 8192, 8192, f32, words, 0)[:2] == (0, 0)
+        assert choice("dx", 8192, 1, 0, 8192, 8192, f32, words, 0)[:2] == (0, 0)
+        assert choice("dw", 8192, 1, 8192, 8192, f32, words)[1] == 0
+
+
+def test_single_tokens_take_the_kernel_for_few_rows(choice):
+    for E, k, d_in, n_j in ((64, 8, 2048, 2048), (8, 2, 256, 128)):
+        assert choice("forward", k, E, 1, n_j, d_in, 0, 1, 0)[::2] == (1, 1)
+    assert choice("forward", 128, 1, 0, 4096, 4096, 0, 1, 0)[0] == 1
+    assert choice("forward", 1024, 1, 0, 4096, 4096, 0, 1, 0)[0] == 0
+
+
+def test_few_weights_and_many_rows_are_summed_in_parts(choice):
+    assert choice("dw", 32768, 1, 1024, 2048, 0, 1)[3] > 1
+    assert choice("dw", 32768, 32, 4096, 4096, 0, 1)[3] == 1
