@@ -194,6 +194,17 @@ void with_lanes(int32_t n_experts, int32_t top_k, F&& f) {
   }
 }
 
+// f(first token, tokens, grid) for as many launches as it takes: one of 2^32 threads and more runs only what is over, and says nothing.
+constexpr int32_t kLaunchTokens = 1 << 25;  // (2^31 threads with 64 lanes a token)
+template <typename F>
+void in_launches(int32_t n_tokens, int lanes, F&& f) {
+  const int32_t each = 256 / lanes;  // of a workgroup
+  for (int64_t t = 0; t < n_tokens; t += kLaunchTokens) {
+    const int32_t n = (int32_t)std::min<int64_t>(n_tokens - t, kLaunchTokens);
+    f(t, n, dim3((unsigned)((n + each - 1) / each)));
+  }
+}
+
 // ------------------------------------------------------------------- sort by expert
 // A stable counting sort.  The entries are cut into one contiguous part per workgroup, and that into one per wavefront; a
 // wavefront counts its entries per expert in LDS, the counts become first places (experts ascending, inside an expert
@@ -371,10 +382,11 @@ extern "C" sptir_status_t sptir_moe_route(const void* logits, int32_t type, int6
   moe_with_type(type, [&](auto v) {
     using T = decltype(v);
     with_lanes(n_experts, top_k, [&](auto l, auto c) {
-      constexpr int kLanes = decltype(l)::value, kTokens = 256 / kLanes;
-      const dim3 grid((n_tokens + kTokens - 1) / kTokens);
-      hipLaunchKernelGGL((k_moe_route<T, kLanes, decltype(c)::value>), grid, dim3(256), 0, (hipStream_t)stream, (const T*)logits, ld_logits,
-                         n_tokens, n_experts, top_k, normalise, experts, weights);
+      constexpr int kLanes = decltype(l)::value;
+      in_launches(n_tokens, kLanes, [&](int64_t t, int32_t n, dim3 grid) {
+        hipLaunchKernelGGL((k_moe_route<T, kLanes, decltype(c)::value>), grid, dim3(256), 0, (hipStream_t)stream, (const T*)logits + t * ld_logits,
+                           ld_logits, n, n_experts, top_k, normalise, experts + t * top_k, weights + t * top_k);
+      });
     });
   });
   SPTIR_HIP(hipGetLastError());
@@ -394,10 +406,12 @@ extern "C" sptir_status_t sptir_moe_route_backward(const void* logits, int32_t t
   moe_with_type(type, [&](auto v) {
     using T = decltype(v);
     with_lanes(n_experts, top_k, [&](auto l, auto c) {
-      constexpr int kLanes = decltype(l)::value, kTokens = 256 / kLanes;
-      const dim3 grid((n_tokens + kTokens - 1) / kTokens);
-      hipLaunchKernelGGL((k_moe_route_backward<T, kLanes, decltype(c)::value>), grid, dim3(256), 0, (hipStream_t)stream, (const T*)logits,
-                         ld_logits, n_tokens, n_experts, top_k, normalise, experts, weights, d_weights, (T*)d_logits, ld_d_logits);
+      constexpr int kLanes = decltype(l)::value;
+      in_launches(n_tokens, kLanes, [&](int64_t t, int32_t n, dim3 grid) {
+        hipLaunchKernelGGL((k_moe_route_backward<T, kLanes, decltype(c)::value>), grid, dim3(256), 0, (hipStream_t)stream,
+                           (const T*)logits + t * ld_logits, ld_logits, n, n_experts, top_k, normalise, experts + t * top_k, weights + t * top_k,
+                           d_weights + t * top_k, (T*)d_logits + t * ld_d_logits, ld_d_logits);
+      });
     });
   });
   SPTIR_HIP(hipGetLastError());

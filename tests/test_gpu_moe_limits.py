@@ -1,0 +1,44 @@
+"""As many tokens and rows as the entry points promise: more workgroups than a launch can have, counts that pass 31 bits."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+def same(a, b, at_once=1 << 27):
+    """a equals b, a piece at a time"""
+    return a.shape == b.shape and all(torch.equal(a[i:i + at_once], b[i:i + at_once]) for i in range(0, a.shape[0], at_once))
+
+
+def repeats(t, few):
+    """whether the rows of t are those of `few` over and over"""
+    n = t.shape[0] // few.shape[0]
+    whole = t[:n * few.shape[0]].view(n, -1)
+    some = max(1, (1 << 27) // whole.shape[1])
+    return (all(bool((whole[i:i + some] == few.reshape(1, -1)).all()) for i in range(0, n, some))
+            and torch.equal(t[n * few.shape[0]:], few[:t.shape[0] - n * few.shape[0]]))
+
+
+# 16 lanes a token, and 64: 2^32 threads and more in one launch
+@pytest.mark.parametrize("T,E,k", [(2 ** 28 + 3, 1, 1), (2 ** 26 + 3, 17, 17)])
+def test_router_of_many_tokens(gpu_lib, T, E, k):
+    print("[moe limits] router", T, E, k, flush=True)
+    gen = torch.Generator().manual_seed(1)
+    few = torch.randn(64, E, generator=gen).to(BF16).cuda()
+    few_dw = torch.randn(64, k, generator=gen).cuda()
+
+    def route(logits, dw):
+        n = logits.shape[0]
+        experts, weights = torch.full((n, k), -7, dtype=torch.int32, device="cuda"), torch.full((n, k), -7.0, device="cuda")
+        d = torch.full((n, E), -7.0, dtype=BF16, device="cuda")
+        gpu_lib.sptir_moe_route(logits, experts, weights, normalise=False)
+        gpu_lib.sptir_moe_route_backward(logits, experts, weights, dw, d, normalise=False)
+        return experts, weights, d
+
+    want = route(few, few_dw)
+    times = -(-T // 64)
+    got = route(few.repeat(times, 1)[:T], few_dw.repeat(times, 1)[:T])
+    torch.cuda.synchronize()
+    for g, w, what in zip(got, want, ("experts", "weights", "d_logits")):
+        assert repeats(g, w), what
