@@ -61,7 +61,17 @@ inline double moe_tiles_estimate(const MoeTileShape& shape, const MoeSizes& s) {
 // (there are wide tiles of 16 bits in words only)
 inline bool moe_wide_pays(const MoeSizes& s) { return s.words && !s.f32 && moe_tiles_estimate(kMoeWide, s) < moe_tiles_estimate(kMoeNarrow, s); }
 
-// The kernel for few rows with 1, 2 and 4 fragments: W is read once for every 16 rows of a fragment (of which the last are half
+// The kernel for few rows: columns of C of a workgroup (where there is one fragment of rows there is one of columns), workgroups, and whether one launch
+// can have them: with 2^32 threads and more it would run only what is over.
+constexpr int kMoeFewThreads = 512;
+constexpr int32_t moe_few_cols(bool gated, int fragments) { return gated || fragments == 1 ? 16 : 32; }
+inline int64_t moe_few_groups(const MoeSizes& s, int fragments) {
+  const int32_t cols = moe_few_cols(s.gated, fragments);
+  return ((s.gated ? s.n_j / 2 : s.n_j) + cols - 1) / cols * moe_most_tiles(s.n_rows, s.n_experts, s.routed, 16 * fragments);
+}
+inline bool moe_few_fits(const MoeSizes& s, int fragments) { return moe_few_groups(s, fragments) < ((int64_t)1 << 32) / kMoeFewThreads; }
+
+// Its time with 1, 2 and 4 fragments (infinite where none fits): W is read once for every 16 rows of a fragment (of which the last are half
 // full on average), at 4.8, 4.0 and 2.7 TB/s as measured for 64 rows of 32 experts (134 MB: 139, 85 and 78 us) and of one
 // (34 MB: 32, 19 and 27 us); with one pass that is 42, 36 and 45 us of 134 MB.  float32 is bound by its products from a few dozen
 // rows on, at 47 TFLOP/s (4006 rows, 777 x 1000: 125 us).  Passes but the first take 2.2 times as long where operands do not lie
@@ -73,12 +83,13 @@ inline double moe_few_estimate(const MoeSizes& s, int32_t* best) {
   const double used = (double)std::min<int64_t>(s.n_rows, s.n_experts);
   const double bytes = used * s.n_j * s.n_r * (s.f32 ? 4 : 2), mean = (double)s.n_rows / used;
   const double rate[] = {4.8e6, 4.0e6, 2.7e6};
-  double least = 0;
+  double least = INFINITY;
   for (int i = 0; i < 3; ++i) {
+    if (!moe_few_fits(s, 1 << i)) continue;
     const double rows = 16 << i;
     const double full = mean / rows, passes = s.routed ? 1 + full * full / (full + 0.5) : std::ceil(full);  // (towards full + 0.5)
     const double us = 5.0 + std::max((s.words ? passes : 1 + 2.2 * (passes - 1)) * bytes / rate[i], s.f32 ? 2.0 * s.n_rows * s.n_j * s.n_r / 47e6 : 0.0);
-    if (i == 0 || us < least) {
+    if (us < least) {
       least = us;
       *best = 1 << i;
     }

@@ -9,7 +9,7 @@
 namespace sptir {
 namespace {
 
-constexpr int kWaves = 8;
+constexpr int kWaves = kMoeFewThreads / 64;
 
 // 16 bytes from anywhere (global memory takes any alignment of an element); elements from `n` on are zeros
 template <typename F, typename T>
@@ -186,11 +186,11 @@ __global__ __launch_bounds__(64 * kWaves) void k_moe_few(MoeProduct p, int32_t a
 
 template <typename T, bool kGated, int kFM, int kFN>
 sptir_status_t launch(int32_t act, const MoeProduct& p, hipStream_t stream) {
-  const int cols = kGated ? 16 : 16 * kFN;
+  const int cols = moe_few_cols(kGated, kFM);
+  static_assert(moe_few_cols(kGated, kFM) == (kGated ? 16 : 16 * kFN), "a workgroup's columns");
   const int32_t out_cols = kGated ? p.n_j / 2 : p.n_j;
   const int64_t j_tiles = (out_cols + cols - 1) / cols;
-  const int64_t groups = j_tiles * moe_most_tiles(p.n_rows, p.n_experts, p.expert_ptr, 16 * kFM);
-  if (groups > (int64_t)INT32_MAX) return SPTIR_ERR_OVERFLOW;
+  const int64_t groups = j_tiles * moe_most_tiles(p.n_rows, p.n_experts, p.expert_ptr, 16 * kFM);  // (as many as fit: moe_choose_forward())
   hipLaunchKernelGGL((k_moe_few<T, kGated, kFM, kFN>), dim3((unsigned)groups), dim3(64 * kWaves), 0, stream, p, act, (int32_t)j_tiles);
   SPTIR_HIP(hipGetLastError());
   return SPTIR_OK;

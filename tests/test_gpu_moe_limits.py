@@ -42,3 +42,13 @@ def test_router_of_many_tokens(gpu_lib, T, E, k):
     torch.cuda.synchronize()
     for g, w, what in zip(got, want, ("experts", "weights", "d_logits")):
         assert repeats(g, w), what
+
+
+# (where the kernel for few rows would take 2^32 threads and more)
+@pytest.mark.parametrize("rows", [2 ** 29 + 5])
+def test_product_of_many_rows(gpu_lib, rows):
+    print("[moe limits] product", rows, flush=True)
+    X = torch.randn(1009, 1, generator=torch.Generator().manual_seed(2)).to(BF16).cuda().repeat(-(-rows // 1009), 1)[:rows]
+    W, Y = torch.full((1, 1), -1.75, dtype=BF16, device="cuda"), torch.zeros(rows, 1, dtype=BF16, device="cuda")
+    gpu_lib.sptir_moe_product(None, X, W, Y)
+    assert repeats(Y, (X[:1009].float() * -1.75).to(BF16))  # (a product of two is rounded once)

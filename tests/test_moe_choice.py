@@ -60,3 +60,12 @@ def test_single_tokens_take_the_kernel_for_few_rows(choice):
 def test_few_weights_and_many_rows_are_summed_in_parts(choice):
     assert choice("dw", 32768, 1, 1024, 2048, 0, 1)[3] > 1
     assert choice("dw", 32768, 32, 4096, 4096, 0, 1)[3] == 1
+
+
+def test_the_kernel_for_few_rows_fits_one_launch(choice):
+    """A launch of 2^32 threads and more runs only a part of them: other kernels take such calls."""
+    for rows, E, routed in ((2 ** 29 + 5, 1, 0), (2 ** 29 + 5, 3, 1), (2 ** 31 - 2, 1, 0), (2 ** 31 - 2, 1024, 1), (3 * 10 ** 8, 1, 0), (2 ** 27 + 1, 1, 0)):
+        for n_j, n_r, gated in ((1, 1, 0), (8, 8, 0), (64, 8, 0), (64, 8, 1), (2 ** 28, 1, 0)):
+            few, _, fragments, _ = choice("forward", rows, E, routed, n_j, n_r, 0, 0, gated)
+            out, cols = (n_j // 2, 16) if gated else (n_j, 16 if fragments == 1 else 32)
+            assert not few or -(-rows // (16 * fragments)) * -(-out // cols) * 512 < 2 ** 32
