@@ -1,5 +1,5 @@
 // Which kernel takes a product of an expert layer, and in which tiles: estimates of its time from sizes, types and alignment.  Plain
-// arithmetic, of the host alone.
+// arithmetic.
 #ifndef SPTIR_MOE_CHOICE_H_
 #define SPTIR_MOE_CHOICE_H_
 
@@ -8,7 +8,16 @@
 #include <algorithm>
 #include <cmath>
 
+#ifdef __HIPCC__
+#define SPTIR_MOE_ANYWHERE __host__ __device__ inline
+#else
+#define SPTIR_MOE_ANYWHERE inline
+#endif
+
 namespace sptir {
+
+// Tiles of `rows` rows that the sorted rows lo .. hi - 1 make.  (There may be 2^31 - 2 of them: what is added to fill the last tile passes 31 bits.)
+SPTIR_MOE_ANYWHERE int moe_tiles_of(int lo, int hi, int rows) { return (int)(((uint32_t)(hi - lo) + (uint32_t)(rows - 1)) / (uint32_t)rows); }
 
 // A call: C[i][j] = sum_r A[i][r] B[j][r] for one expert at a time (forward: n_j rows of W, swiglu's both halves, n_r inputs; dx: n_j
 // inputs, n_r outputs).

@@ -40,7 +40,7 @@ __device__ inline bool find_tile(const MoeProduct& p, int rows, int64_t tile, Mo
       lo = p.expert_ptr[e];
       hi = e < p.n_experts ? p.expert_ptr[e + 1] : (int)p.n_rows;
     }
-    const int tiles = (hi - lo + rows - 1) / rows;
+    const int tiles = moe_tiles_of(lo, hi, rows);
     int sum = tiles;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {

@@ -37,7 +37,7 @@ __device__ inline uint32_t moe_fill_table(const MoeProduct& p, int rows, const M
       int lo = (int)p.n_rows, hi = (int)p.n_rows;
       if (e <= p.n_experts) lo = p.expert_ptr[e];
       if (e < p.n_experts) hi = p.expert_ptr[e + 1];
-      int sum = (hi - lo + rows - 1) / rows;
+      int sum = moe_tiles_of(lo, hi, rows);
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
         const int o = __shfl_up(sum, d);

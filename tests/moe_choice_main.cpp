@@ -1,6 +1,6 @@
 // Which kernel takes a product of an expert layer (csrc/moe_choice.h, compiled alone), for test_moe_choice.py.  Reads lines
 //   "forward|dx n_rows n_experts routed n_j n_r f32 words gated"  or  "dw n_rows n_experts d_in d_z f32 words"
-// and prints "few wide fragments parts" of each.
+// and prints "few wide fragments parts" of each; or "tiles lo hi rows", and prints their number.
 #include <stdio.h>
 #include <string.h>
 
@@ -11,7 +11,11 @@ int main() {
   while (scanf("%15s", op) == 1) {
     long long n_rows;
     int experts, f32, words;
-    if (!strcmp(op, "dw")) {
+    if (!strcmp(op, "tiles")) {
+      int lo, hi, rows;
+      if (scanf("%d %d %d", &lo, &hi, &rows) != 3) return 1;
+      printf("%d\n", sptir::moe_tiles_of(lo, hi, rows));
+    } else if (!strcmp(op, "dw")) {
       int d_in, d_z;
       if (scanf("%lld %d %d %d %d %d", &n_rows, &experts, &d_in, &d_z, &f32, &words) != 6) return 1;
       const int parts = sptir::moe_dw_parts(n_rows, experts, d_in, d_z);

@@ -52,3 +52,45 @@ def test_product_of_many_rows(gpu_lib, rows):
     W, Y = torch.full((1, 1), -1.75, dtype=BF16, device="cuda"), torch.zeros(rows, 1, dtype=BF16, device="cuda")
     gpu_lib.sptir_moe_product(None, X, W, Y)
     assert repeats(Y, (X[:1009].float() * -1.75).to(BF16))  # (a product of two is rounded once)
+
+
+# all but five rows of the last expert, and of no expert
+@pytest.mark.parametrize("E", [2, 1])
+def test_experts_of_as_many_rows_as_there_may_be(gpu_lib, E):
+    n = 2 ** 31 - 2
+    print("[moe limits] rows", n, E, flush=True)
+    ptr = torch.tensor([0, 5, n][:E + 1], dtype=torch.int32, device="cuda")
+    unread = torch.empty(n, dtype=torch.int32, device="cuda")
+    r = gpu_lib.MoeRouting(n, 1, E, ptr, unread, unread)
+    few = torch.randn(1009, 1, generator=torch.Generator().manual_seed(3)).to(BF16).cuda()
+    X = few.repeat(-(-n // 1009), 1)[:n]
+    W = torch.tensor([[[0.5]], [[-3.0]]][:E], dtype=BF16, device="cuda")
+    Y = torch.full((n, 1), 7.0, dtype=BF16, device="cuda")
+    last = -3.0 if E == 2 else 0.0
+    for call in (gpu_lib.sptir_moe_product, gpu_lib.sptir_moe_product_dx):
+        Y.fill_(7.0)
+        call(r, X, W, Y)
+        assert torch.equal(Y[:5], (few[:5].float() * 0.5).to(BF16))
+        assert repeats(Y[1009:], (few.float() * last).to(BF16))
+        assert torch.equal(Y[5:1009], (few[5:].float() * last).to(BF16))
+
+
+def test_entries_of_as_many_tokens_as_there_may_be(gpu_lib):
+    """Sorted, there and back, a column wide: token t goes to expert t % 2."""
+    n = 2 ** 31 - 2
+    print("[moe limits] entries", n, flush=True)
+    half = n // 2
+    experts = torch.tensor([[0], [1]], dtype=torch.int32, device="cuda").repeat(half, 1)
+    r = gpu_lib.sptir_moe_sort(experts, 2)
+    assert r.expert_ptr.tolist() == [0, half, n]
+    for which in range(2):
+        places, entries = r.slot_of.view(half, 2)[:, which], r.entry_of[which * half:(which + 1) * half]
+        for i in range(0, half, 1 << 28):
+            want = torch.arange(i, min(i + (1 << 28), half), dtype=torch.int32, device="cuda")
+            assert torch.equal(places[i:i + (1 << 28)], want + which * half) and torch.equal(entries[i:i + (1 << 28)], want * 2 + which)
+    X = torch.randn(1009, 1, generator=torch.Generator().manual_seed(4)).to(BF16).cuda().repeat(-(-n // 1009), 1)[:n]
+    Xs, Y = torch.zeros_like(X), torch.zeros_like(X)
+    gpu_lib.sptir_moe_gather(r, X, Xs)
+    assert same(Xs[:half], X[::2]) and same(Xs[half:], X[1::2])
+    gpu_lib.sptir_moe_combine(r, Xs, Y)
+    assert same(Y, X)

@@ -69,3 +69,10 @@ def test_the_kernel_for_few_rows_fits_one_launch(choice):
             few, _, fragments, _ = choice("forward", rows, E, routed, n_j, n_r, 0, 0, gated)
             out, cols = (n_j // 2, 16) if gated else (n_j, 16 if fragments == 1 else 32)
             assert not few or -(-rows // (16 * fragments)) * -(-out // cols) * 512 < 2 ** 32
+
+
+@pytest.mark.parametrize("rows", [16, 32, 64, 128, 256])
+def test_tiles_of_as_many_rows_as_there_may_be(choice, rows):
+    most = 2 ** 31 - 2
+    for lo, hi in ((0, most), (1, most), (0, most - rows), (5, most), (7, 7), (most, most), (0, 1), (3, 3 + rows), (3, 4 + rows)):
+        assert choice("tiles", lo, hi, rows) == (-(-(hi - lo) // rows),)
