@@ -98,6 +98,7 @@ extern "C" sptir_status_t sptir_moe_product_dx(const sptir_moe_routing_t* routin
 
 extern "C" int64_t sptir_moe_product_dw_workspace(int64_t n_rows, int32_t n_experts, int32_t d_in, int32_t d_z) {
   if (n_rows <= 0 || n_experts <= 0 || d_in < 0 || d_z <= 0) return 0;
+  if (n_experts > kMoeMaxExperts || d_in > INT32_MAX / 4 || d_z > INT32_MAX / 4) return 0;  // (the call is refused)
   return moe_dw_workspace(moe_dw_parts(n_rows, n_experts, d_in, d_z), n_experts, d_in, d_z);
 }
 

@@ -7,6 +7,7 @@ import pytest
 
 import moe_wide_shapes as wide
 from paper_2207_04606_amd import build as sptir_build
+from paper_2207_04606_amd import moe
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -76,3 +77,11 @@ def test_tiles_of_as_many_rows_as_there_may_be(choice, rows):
     most = 2 ** 31 - 2
     for lo, hi in ((0, most), (1, most), (0, most - rows), (5, most), (7, 7), (most, most), (0, 1), (3, 3 + rows), (3, 4 + rows)):
         assert choice("tiles", lo, hi, rows) == (-(-(hi - lo) // rows),)
+
+
+def test_no_workspace_for_sizes_that_are_refused():
+    need = moe._library().sptir_moe_product_dw_workspace
+    most = 2 ** 31 - 1
+    for sizes in ((10 ** 6, 1, 64, most), (10 ** 6, 1, most, 64), (10 ** 6, 1, most, most), (10 ** 6, 1, 64, most // 4 + 1), (2 ** 62, most, 64, 64), (10 ** 6, 1025, 1, 1)):
+        assert need(*sizes) == 0
+    assert need(10 ** 6, 1, 64, 64) > 0
