@@ -36,7 +36,7 @@ __device__ inline float act_phi(float z) {
     const float half = 0.5f * t * act_exp<T>(s - x * x);
     return z < 0.f ? half : 1.f - half;
   }
-  return 0.5f * (1.f + erff(z * 0.70710678118654752f));
+  return 0.5f * erfcf(z * -0.70710678118654752f);  // (1 + erf would leave no digit below -5)
 }
 
 // y of one z (not swiglu, which takes two)
