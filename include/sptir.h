@@ -509,7 +509,8 @@ sptir_status_t sptir_rgms_destroy(sptir_rgms_t* rgms); /* NULL is accepted */
  */
 typedef enum { SPTIR_F32 = 0, SPTIR_F16 = 1, SPTIR_BF16 = 2 } sptir_type_t;
 
-/* How an expert's product z becomes y.  gelu is the one with erf; swiglu takes two halves of z: silu(z[0..n)) * z[n..2n). */
+/* How an expert's product z becomes y.  gelu is the one with erf; swiglu takes two halves of z: silu(z[0..n)) * z[n..2n).
+ * A z that is NaN makes y NaN. */
 typedef enum {
   SPTIR_ACT_NONE = 0,
   SPTIR_ACT_RELU = 1,

@@ -42,7 +42,7 @@ __device__ inline float act_phi(float z) {
 // y of one z (not swiglu, which takes two)
 template <int kAct, typename T>
 __device__ inline float act_value(float z) {
-  if constexpr (kAct == SPTIR_ACT_RELU) return z > 0.f ? z : 0.f;
+  if constexpr (kAct == SPTIR_ACT_RELU) return z <= 0.f ? 0.f : z;  // (NaN stays NaN)
   if constexpr (kAct == SPTIR_ACT_GELU) return z * act_phi<T>(z);
   if constexpr (kAct == SPTIR_ACT_SILU) return z * act_sigmoid<T>(z);
   return z;
@@ -51,7 +51,7 @@ __device__ inline float act_value(float z) {
 // d times the derivative at z
 template <int kAct, typename T>
 __device__ inline float act_slope(float d, float z) {
-  if constexpr (kAct == SPTIR_ACT_RELU) return z > 0.f ? d : 0.f;
+  if constexpr (kAct == SPTIR_ACT_RELU) return z <= 0.f ? 0.f : d;
   if constexpr (kAct == SPTIR_ACT_GELU)  // Phi(z) + z phi(z); 1 / sqrt(2 pi)
     return d * (act_phi<T>(z) + z * act_exp<T>(-0.5f * z * z) * 0.39894228040143268f);
   if constexpr (kAct == SPTIR_ACT_SILU) {
