@@ -501,9 +501,9 @@ sptir_status_t sptir_rgms_destroy(sptir_rgms_t* rgms); /* NULL is accepted */
 /*
  * A mixture-of-experts layer: the relational operator above with the router's choice of experts as its relations, for
  * which a handle would have to be built anew at every step.  T = n_tokens tokens choose k = top_k of E = n_experts experts
- * each; entry t * k + j is choice j of token t, and there are N = T * k < 2^31 entries.  An entry whose expert is outside
- * 0 .. E - 1 is dropped: it contributes nothing anywhere.  Limits of all entry points (UNSUPPORTED beyond): E <= 1024,
- * k <= 64.  They only enqueue work on `stream`, allocate nothing, may be captured, and give the same bits for the same
+ * each; entry t * k + j is choice j of token t, and there are N = T * k < 2^31 - 1 entries (OVERFLOW beyond).  An entry
+ * whose expert is outside 0 .. E - 1 is dropped: it contributes nothing anywhere.  Limits of all entry points (UNSUPPORTED
+ * beyond): E <= 1024, k <= 64.  They only enqueue work on `stream`, allocate nothing, may be captured, and give the same bits for the same
  * inputs (no atomics on values).  Matrices are row-major with a row stride (ld, in elements, at least the row's length);
  * none of them may overlap an output unless it is said so.  All pointers are device pointers.
  */
@@ -522,7 +522,8 @@ typedef enum {
 /*
  * The entries in the order of the experts (sptir_moe_sort), ascending inside an expert: those of expert e are the rows
  * expert_ptr[e] .. expert_ptr[e + 1) of every matrix that is "in sorted order" (N rows).  Rows from expert_ptr[E] on
- * belong to no entry: where an operator writes a matrix in sorted order it fills them with zeros, and it never reads them.
+ * belong to no entry: where an operator writes a matrix in sorted order it fills them with zeros, and what they hold reaches
+ * nothing.
  */
 typedef struct {
   int32_t n_tokens, top_k, n_experts;
@@ -577,7 +578,7 @@ sptir_status_t sptir_moe_combine_backward(const sptir_moe_routing_t* routing, in
  * d_out, or 2 * d_out for swiglu.  routing NULL: one expert and n_rows rows, the ordinary product of a dense layer.
  * bias, residual and pre may be NULL; `pre` receives z, for the gradient of the activation; residual may be Y itself.
  * Products are summed in float32 (float32 ones with the float32 matrix instructions) and rounded once.
- * Rows that are in no expert's range are not read: what they hold (NaN) reaches nothing.
+ * What rows in no expert's range hold (NaN) reaches nothing.
  */
 typedef struct {
   int32_t struct_size; /* sizeof(sptir_moe_product_t) */
@@ -622,8 +623,8 @@ sptir_status_t sptir_moe_product_dx(const sptir_moe_routing_t* routing, const sp
 
 /*
  * dW[e] = sum over the rows s of expert e of dZ[s] x^T and db[e] = sum of dZ[s] (db may be NULL); zeros for an expert
- * without rows.  `workspace`: sptir_moe_product_dw_workspace bytes (0: may be NULL) at a multiple of 16, free again once the
- * work is done: where dW is small and rows are many, they are summed in parts, which are added up in their order.
+ * without rows.  `workspace`: sptir_moe_product_dw_workspace bytes (0, as for sizes that are refused: may be NULL) at a
+ * multiple of 16, free again once the work is done: where dW is small and rows are many, they are summed in parts, which are added up in their order.
  */
 typedef struct {
   int32_t struct_size;

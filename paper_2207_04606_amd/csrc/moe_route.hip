@@ -207,7 +207,7 @@ void in_launches(int32_t n_tokens, int lanes, F&& f) {
 
 // ------------------------------------------------------------------- sort by expert
 // A stable counting sort.  The entries are cut into one contiguous part per workgroup, and that into one per wavefront; a
-// wavefront counts its entries per expert in LDS, the counts become first places (experts ascending, inside an expert
+// wavefront counts its entries per expert in LDS, the counts (whole numbers: the order of their additions changes nothing) become first places (experts ascending, inside an expert
 // parts ascending), and the wavefront then places its entries in order, 64 at a time: those of one expert are found with a
 // ballot per bit of the expert's number.  With more than one workgroup the counts of all of them come from a launch before.
 // Bound by latency: every step waits for the one before.  (131,072 entries, 128 experts: counts 3.3 us, places 9.8; 8 entries, in one

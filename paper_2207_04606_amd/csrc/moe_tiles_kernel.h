@@ -1,11 +1,17 @@
 // The experts' products in tiles: operands from memory to LDS, matrix instructions from there.  (Compiled once for every
 // product, moe_tiles_forward.hip, moe_tiles_dx.hip and moe_tiles_dw.hip.)
 //
-// A workgroup keeps a tile of C in registers and adds up 128 bytes of r a step.  What bounds it is LDS: a wide tile's eight
-// wavefronts read (128 + 64) x 128 bytes each for 2^15 x 64 multiply-adds, 1536 clocks of LDS beside 2048 of matrix instructions;
-// with long rows 8192 x 8192 x 8192 of bf16 take 900 us, 1220 TFLOP/s (a large library product reaches 1290), 8192 x 4096 x 4096
+// A workgroup keeps a tile of C in registers and adds up 128 bytes of r a step.  A step of a wide tile is 2048 clocks of matrix
+// instructions beside 768 of LDS, by its counter: eight wavefronts read (128 + 64) x 128 bytes each for 2^15 x 64 multiply-adds.  What bounds
+// it are the waits: of a CU's clocks matrix instructions fill 52 to 56 % (8192 x 4096 x 4096; 8192 x 8192 rows of prompts), a wavefront waits a third
+// of its time, at the step's barrier and for its reads.
+// With long rows 8192 x 8192 x 8192 of bf16 take 900 us, 1220 TFLOP/s (a large library product reaches 1290), 8192 x 4096 x 4096
 // 250 us, 1100, the gradients 1070 and 1030.  With short ones (r = 1024) the step's loads are not there in time, since all
 // workgroups ask memory for new operands at once, and the epilogue is a sixth of the tile: 32,768 rows, 1024 x 2048, 140 us, 980.
+// The gradients of 16 bits (39, 30 and 31 % matrix instructions in forward, dX and dW of those sizes with uneven experts) lose more: the compiler takes
+// the transposing LDS reads to need the loads that write LDS and waits for all of these before the first such read of a step (dW) or of its
+// second half (dX), so that a step's loads have a part of a step to arrive in, not a whole one; 4 to 8 % of the clocks are LDS bank conflicts; and the wide
+// kernels spill at the change of tile (dW 20 registers, 28 with db; dX 10 to 16), where every reload waits for all loads too.
 // float32 is bound by its instructions: 4096 x 4096 x 4096 1040 us, 132 TFLOP/s (a library product: 150).  Operands that do not
 // lie in words pass through registers: 540 TFLOP/s in 16 bits.  Measured and left out: tiles of 64 x 64 and 64 x 128 (not faster
 // where the others are few, 1.5 times slower where many), four steps in LDS for a workgroup alone on its CU (no faster: it waits for
@@ -212,7 +218,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
     });
   };
   // (dw) The entries whose tokens' rows of X a step loads, asked for a step earlier: to wait for one that has just been asked
-  // for would be to wait for all loads before it.
+  // for is to wait for all loads before it.  (So it is with a tile's second step: its entries are asked for between the first one's loads and its own.)
   int32_t entry[kOp == kMoeDw ? kLoadsB : 1] = {};
   auto ask = [&](int step) __attribute__((always_inline)) {
     if constexpr (kOp == kMoeDw) {
