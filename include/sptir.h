@@ -548,6 +548,35 @@ sptir_status_t sptir_moe_route_backward(const void* logits, int32_t type, int64_
                                         const float* weights, const float* d_weights, void* d_logits,
                                         int64_t ld_d_logits, void* stream);
 
+/*
+ * The router with scores of another kind.  With s the softmax of a token's logits or their sigmoids 1 / (1 + exp(-l)), and c = s + bias
+ * (bias NULL: s), both in float64:
+ *   An expert is a candidate unless its logit or its c is -inf or NaN.  The experts are n_groups (at most 64, UNSUPPORTED beyond; a divisor of
+ *   E) groups of neighbours; a group's score is the sum of the group_top (1 or 2) largest c of its candidates, of as many as there are.  The top_groups groups
+ *   with the largest scores stay (ties: the lower number; never one without a candidate).  experts[t * k + j] is the candidate with the j-th
+ *   largest c in them (ties: the lower id), -1 with weight 0 where none is left.  k is at most the number of experts of top_groups groups.
+ *   weights = scale * s, normalised: scale * s / the sum of the token's k chosen s.
+ * The bias moves the choice and no weight, and has no gradient: a program raises it for experts that got too few entries (the differences
+ * of expert_ptr) and lowers it for others.  Sigmoids so small that float32 has none are normalised by their exponents: no 0 / 0.
+ * A NaN or +inf that the sum of a softmax runs over makes the weights of its token NaN.  scale is finite.
+ */
+typedef enum { SPTIR_SCORE_SOFTMAX = 0, SPTIR_SCORE_SIGMOID = 1 } sptir_score_t;
+typedef struct {
+  int32_t struct_size; /* sizeof(sptir_moe_scoring_t) */
+  int32_t score, normalise;
+  int32_t n_groups, top_groups, group_top; /* 1, 1, 1: no groups */
+  float scale;
+  const float* bias; /* [E] */
+} sptir_moe_scoring_t;
+sptir_status_t sptir_moe_route_groups(const void* logits, int32_t type, int64_t ld_logits, int32_t n_tokens, int32_t n_experts,
+                                      int32_t top_k, const sptir_moe_scoring_t* scoring, int32_t* experts, float* weights,
+                                      void* stream);
+/* The gradient of the logits; scoring, experts and weights as above (bias and groups have no part in it).  d_weights of a choice -1 is not read as a value. */
+sptir_status_t sptir_moe_route_groups_backward(const void* logits, int32_t type, int64_t ld_logits, int32_t n_tokens,
+                                               int32_t n_experts, int32_t top_k, const sptir_moe_scoring_t* scoring,
+                                               const int32_t* experts, const float* weights, const float* d_weights,
+                                               void* d_logits, int64_t ld_d_logits, void* stream);
+
 /* Sorts the entries by expert (stable).  The arrays are those of sptir_moe_routing_t; `workspace` has
  * sptir_moe_sort_workspace bytes (0 for small N: may then be NULL) and is free again once the call's work is done. */
 int64_t sptir_moe_sort_workspace(int64_t n_entries, int32_t n_experts);
@@ -601,6 +630,34 @@ typedef struct {
 sptir_status_t sptir_moe_product(const sptir_moe_routing_t* routing, const sptir_moe_product_t* product, void* stream);
 
 /*
+ * The experts' products of 8-bit integers.  X and W of `product` hold int8 values (any, -128 too); x and W[e] are these times x_scales[row of X]
+ * and w_scales[e * w_scales_stride + row of W[e]]: a scale for each token and one for each output channel (swiglu: 2 * d_out).
+ * `type` is that of Y, bias, residual and pre.  Sums are whole numbers without rounding, d_in at most 131071 (UNSUPPORTED beyond); z is
+ * (the sum * x's scale) * W's scale + bias in float32.  Everything else as sptir_moe_product.
+ */
+sptir_status_t sptir_moe_product_int8(const sptir_moe_routing_t* routing, const sptir_moe_product_t* product, const float* x_scales,
+                                      const float* w_scales, int64_t w_scales_stride, void* stream);
+/* Rows as the above takes them: scales[r] = the largest |X[r]| / 127, and Q[r] the whole numbers nearest to X[r] / scales[r] (ties to even;
+ * -127 .. 127).  A row of zeros: scale 0, and so where float32 has no smaller number; a row with a NaN or an infinity: scale NaN and codes 0. */
+sptir_status_t sptir_moe_quantise(int32_t type, int32_t width, int64_t n_rows, const void* X, int64_t ldx, int8_t* Q, int64_t ldq,
+                                  float* scales, void* stream);
+
+/*
+ * Activations kept in 8 bits from the forward pass to the backward pass.  32 columns of a row (the last ones of it: fewer) share an exponent:
+ *   X ~ Q * 2^(exponent - 127),  Q = the nearest whole number of -127 .. 127, ties to even,
+ * the exponent the smallest, 1 at least, with which the largest of the 32 rounds to 127 at most.  Exponents: [n_rows, ceil(width / 32)] bytes
+ * with a row stride.  What is kept is a number of X's type exactly, so that products read it without another rounding: float16's
+ * exponents begin at 103 (2^-24), and a code of 64 whose value would be past the type's range is 63.  A NaN or an infinity makes
+ * its 32 columns NaN (exponent 255).
+ */
+sptir_status_t sptir_moe_pack(int32_t type, int32_t width, int64_t n_rows, const void* X, int64_t ldx, int8_t* Q, int64_t ldq,
+                              uint8_t* exponents, int64_t ld_exponents, void* stream);
+/* Y = act(what Q and the exponents stand for) of `type`, rounded once.  swiglu: rows of width / 2.  With the activation the rows that an expert's
+ * next product took (x of sptir_moe_product_dw) come from the z of the last one, and need not be kept themselves. */
+sptir_status_t sptir_moe_unpack(int32_t type, int32_t activation, int32_t width, int64_t n_rows, const int8_t* Q, int64_t ldq,
+                                const uint8_t* exponents, int64_t ld_exponents, void* Y, int64_t ldy, void* stream);
+
+/*
  * dX[s] = W[e]^T dZ[s], in sorted order (sptir_moe_combine without weights brings it to the tokens).  With an activation
  * the result is multiplied by its derivative at `pre`, the z of the product whose y was this product's x, so that it is
  * that product's dZ: [rows, d_in], or [rows, 2 * d_in] for swiglu, as pre.  pre is not read without an activation.
@@ -620,6 +677,9 @@ typedef struct {
   int64_t ld_dx;
 } sptir_moe_product_dx_t;
 sptir_status_t sptir_moe_product_dx(const sptir_moe_routing_t* routing, const sptir_moe_product_dx_t* product, void* stream);
+/* The same where pre is kept in 8 bits (sptir_moe_pack of its `type`): `pre` has the codes, ld_pre is their stride. */
+sptir_status_t sptir_moe_product_dx_packed(const sptir_moe_routing_t* routing, const sptir_moe_product_dx_t* product,
+                                           const uint8_t* exponents, int64_t ld_exponents, void* stream);
 
 /*
  * dW[e] = sum over the rows s of expert e of dZ[s] x^T and db[e] = sum of dZ[s] (db may be NULL); zeros for an expert
@@ -644,6 +704,11 @@ typedef struct {
 } sptir_moe_product_dw_t;
 int64_t sptir_moe_product_dw_workspace(int64_t n_rows, int32_t n_experts, int32_t d_in, int32_t d_z);
 sptir_status_t sptir_moe_product_dw(const sptir_moe_routing_t* routing, const sptir_moe_product_dw_t* product, void* stream);
+/* The same where X is kept in 8 bits (sptir_moe_pack of its `type`): `X` has the codes, ldx is their stride; `workspace`: sptir_moe_product_dw_packed_workspace
+ * bytes (x_rows: the rows of X, n_tokens with `gather`), in which x is brought back to its type. */
+int64_t sptir_moe_product_dw_packed_workspace(int32_t type, int64_t x_rows, int64_t n_rows, int32_t n_experts, int32_t d_in, int32_t d_z);
+sptir_status_t sptir_moe_product_dw_packed(const sptir_moe_routing_t* routing, const sptir_moe_product_dw_t* product,
+                                           const uint8_t* exponents, int64_t ld_exponents, void* stream);
 
 /* Releases the handle and its device arrays.  NULL is accepted.  Under the default allocator it waits for the device, as
  * hipFree does, and like hipFree it may be called while a stream is captured in relaxed mode only. */

@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsptir.so")
 SOURCES = ["api.hip", "builder.hip", "order.hip", "spmm.hip", "spmm_slices.hip", "spmm_csr.hip", "sddmm.hip", "sddmm_slices.hip", "search.hip", "rgms.hip", "roof.hip",
            "moe_route.hip", "moe_rows.hip", "moe_product.hip", "moe_few.hip", "moe_tiles_forward.hip",
-           "moe_tiles_dx.hip", "moe_tiles_dw.hip"]
+           "moe_tiles_dx.hip", "moe_tiles_dw.hip", "moe_route_groups.hip", "moe_rows8.hip", "moe_tiles_int8.hip", "moe_tiles_dx_kept.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -71,15 +71,17 @@ __device__ inline void write_word(T* p, u32x4 w, int many) {
   }
 }
 
-// whether rows of `width` elements can be taken in 16-byte words
-inline bool moe_words(int32_t type, int64_t width, std::initializer_list<const void*> data, std::initializer_list<int64_t> ld) {
-  const int per = 16 / moe_type_bytes(type);
+// whether rows of `width` elements, `per` of them 16 bytes, can be taken in 16-byte words
+inline bool moe_words_of(int per, int64_t width, std::initializer_list<const void*> data, std::initializer_list<int64_t> ld) {
   if (width % per) return false;
   for (const void* p : data)
     if ((uintptr_t)p & 15) return false;
   for (int64_t l : ld)
     if (l % per) return false;
   return true;
+}
+inline bool moe_words(int32_t type, int64_t width, std::initializer_list<const void*> data, std::initializer_list<int64_t> ld) {
+  return moe_words_of(16 / moe_type_bytes(type), width, data, ld);
 }
 
 }  // namespace sptir

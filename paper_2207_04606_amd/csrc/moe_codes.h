@@ -1,0 +1,55 @@
+// Rows kept in 8 bits: whole numbers of -127 .. 127 with a power of two for every 32 columns of a row.
+#ifndef SPTIR_MOE_CODES_H_
+#define SPTIR_MOE_CODES_H_
+
+#include "moe.h"
+
+namespace sptir {
+
+constexpr int kMoeBlock = 32;  // columns that share an exponent
+inline int64_t moe_blocks(int64_t width) { return (width + kMoeBlock - 1) / kMoeBlock; }
+
+// The power of two that an exponent's byte stands for; 255: a NaN, whatever the codes.
+__device__ inline float code_unit(uint32_t exponent) {
+  return exponent == 255 ? __builtin_nanf("") : __builtin_bit_cast(float, exponent << 23);
+}
+__device__ inline float code_of(uint32_t word, int byte) { return (float)(int8_t)(word >> 8 * byte); }
+
+// The first `many` of kN codes, zeros behind them
+template <int kN>
+struct Codes {
+  uint32_t w[kN / 4];
+  __device__ inline float at(int i) const { return code_of(w[i / 4], i % 4); }
+};
+template <int kN>
+__device__ inline Codes<kN> read_codes(const int8_t* p, int many) {
+  Codes<kN> c = {};
+  if (many >= kN) {
+    __builtin_memcpy(c.w, p, kN);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+      if (i < many) c.w[i / 4] |= (uint32_t)(uint8_t)p[i] << i % 4 * 8;
+  }
+  return c;
+}
+
+// kN values of a row from column c on, `many` of which are there.  They may lie in two blocks (kOne: they do not).
+template <int kN, bool kOne>
+__device__ inline void read_kept(const int8_t* row, const uint8_t* exponents, int64_t c, int many, float (&v)[kN]) {
+  const Codes<kN> codes = read_codes<kN>(row + c, many);
+  const float unit = code_unit(exponents[c / kMoeBlock]);
+  float next = unit;
+  if (!kOne && many > 0) next = code_unit(exponents[(c + (many < kN ? many : kN) - 1) / kMoeBlock]);
+  const int over = kMoeBlock - (int)(c % kMoeBlock);  // the first of the next block
+#pragma unroll
+  for (int i = 0; i < kN; ++i) v[i] = codes.at(i) * (kOne || i < over ? unit : next);
+}
+
+// (moe_rows8.hip) sptir_moe_unpack, its arguments checked
+sptir_status_t moe_unpack(int32_t type, int32_t act, int32_t width, int64_t n_rows, const int8_t* Q, int64_t ldq, const uint8_t* exponents,
+                          int64_t ld_exponents, void* Y, int64_t ldy, hipStream_t stream);
+
+}  // namespace sptir
+
+#endif  // SPTIR_MOE_CODES_H_

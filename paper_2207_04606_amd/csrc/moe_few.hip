@@ -20,7 +20,7 @@ __device__ inline F read_frag(const T* p, int64_t n) {
     __builtin_memcpy(&f, p, 16);
   } else {
 #pragma unroll
-    for (int i = 0; i < kN; ++i) f[i] = i < n ? p[i] : from_float<T>(0.f);
+    for (int i = 0; i < kN; ++i) f[i] = i < n ? p[i] : (T)0;
   }
   return f;
 }
@@ -99,22 +99,24 @@ __device__ inline void clear(const MoeProduct& p, int64_t i, int32_t j) {
   }
 }
 
-// kFM, kFN: fragments of 16 rows and of 16 columns (gated: one of gates, one of what goes with them)
-template <typename T, bool kGated, int kFM, int kFN>
+// T: the operands' type, O that of everything else (T of 8-bit integers: as in k_moe_tiles).  kFM, kFN: fragments of 16 rows and of 16 columns (gated: one of gates, one of what goes with them)
+template <typename T, bool kGated, int kFM, int kFN, typename O = T>
 __global__ __launch_bounds__(64 * kWaves) void k_moe_few(MoeProduct p, int32_t act, int32_t j_tiles) {
   static_assert(!kGated || kFN == 2, "a gate has its pair beside it");
+  constexpr bool kInt8 = std::is_same_v<T, int8_t>;
   constexpr int kCols = kGated ? 16 : 16 * kFN, kN = 16 / sizeof(T), kStep = 8 * kN;  // of r, a wavefront's turn: 128 bytes
   constexpr int kTurns = kFM == 1 ? 4 : kFM == 2 ? 2 : 1;
   using M = Mma<T>;
   using Frag = typename M::Frag;
-  __shared__ f32x4 part[kWaves][kFM * kFN][64];
+  using Acc = typename M::Acc;
+  __shared__ Acc part[kWaves][kFM * kFN][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, q = lane >> 4;
   const int32_t out_cols = kGated ? p.n_j / 2 : p.n_j;
   MoeTile t;
   if (!find_tile(p, 16 * kFM, blockIdx.x / j_tiles, &t)) return;
   const int32_t j0 = (int32_t)(blockIdx.x % j_tiles) * kCols;
   const bool none = t.expert == p.n_experts;
-  f32x4 acc[kFM][kFN] = {};
+  Acc acc[kFM][kFN] = {};
   if (!none) {
     const T* x[kFM];
     const T* w[kFN];
@@ -162,7 +164,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_moe_few(MoeProduct p, int32_t a
   for (int n = threadIdx.x; n < kPieces * 64; n += 64 * kWaves) {
     const int piece = n >> 6, l = n & 63;  // (the lane that these sums come from)
     const int f = kGated ? piece : piece / kFN, g = kGated ? 0 : piece % kFN;
-    f32x4 sum = part[0][f * kFN + g][l], pair = kGated ? part[0][f * kFN + 1][l] : sum;
+    Acc sum = part[0][f * kFN + g][l], pair = kGated ? part[0][f * kFN + 1][l] : sum;
 #pragma unroll
     for (int v = 1; v < kWaves; ++v) {
       sum += part[v][f * kFN + g][l];
@@ -170,48 +172,68 @@ __global__ __launch_bounds__(64 * kWaves) void k_moe_few(MoeProduct p, int32_t a
     }
     const int64_t i = t.first + 16 * f + (l & 15);
     if (i >= t.end) continue;
+    float of_row = 1.f;
+    if constexpr (kInt8)
+      if (!none) of_row = p.a_scales[x_row(p, i)];
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
       const int32_t j = j0 + 16 * g + (l >> 4) * 4 + v;
       if (j >= out_cols) continue;
-      if (none) clear<T, kGated>(p, i, j);
-      else if (kGated) emit_gated<T>(p, t.expert, i, j, sum[v], pair[v]);
-      else if (act == SPTIR_ACT_RELU) emit<T, SPTIR_ACT_RELU>(p, t.expert, i, j, sum[v]);
-      else if (act == SPTIR_ACT_GELU) emit<T, SPTIR_ACT_GELU>(p, t.expert, i, j, sum[v]);
-      else if (act == SPTIR_ACT_SILU) emit<T, SPTIR_ACT_SILU>(p, t.expert, i, j, sum[v]);
-      else emit<T, SPTIR_ACT_NONE>(p, t.expert, i, j, sum[v]);
+      float z = (float)sum[v], up = (float)pair[v];
+      if constexpr (kInt8) {
+        if (!none) {
+          const float* of_column = p.b_scales + t.expert * p.b_scales_stride + j;
+          z = z * of_row * of_column[0];
+          if (kGated) up = up * of_row * of_column[out_cols];
+        }
+      }
+      if (none) clear<O, kGated>(p, i, j);
+      else if (kGated) emit_gated<O>(p, t.expert, i, j, z, up);
+      else if (act == SPTIR_ACT_RELU) emit<O, SPTIR_ACT_RELU>(p, t.expert, i, j, z);
+      else if (act == SPTIR_ACT_GELU) emit<O, SPTIR_ACT_GELU>(p, t.expert, i, j, z);
+      else if (act == SPTIR_ACT_SILU) emit<O, SPTIR_ACT_SILU>(p, t.expert, i, j, z);
+      else emit<O, SPTIR_ACT_NONE>(p, t.expert, i, j, z);
     }
   }
 }
 
-template <typename T, bool kGated, int kFM, int kFN>
+template <typename T, bool kGated, int kFM, int kFN, typename O>
 sptir_status_t launch(int32_t act, const MoeProduct& p, hipStream_t stream) {
   const int cols = moe_few_cols(kGated, kFM);
   static_assert(moe_few_cols(kGated, kFM) == (kGated ? 16 : 16 * kFN), "a workgroup's columns");
   const int32_t out_cols = kGated ? p.n_j / 2 : p.n_j;
   const int64_t j_tiles = (out_cols + cols - 1) / cols;
   const int64_t groups = j_tiles * moe_most_tiles(p.n_rows, p.n_experts, p.expert_ptr, 16 * kFM);  // (as many as fit: moe_choose_forward())
-  hipLaunchKernelGGL((k_moe_few<T, kGated, kFM, kFN>), dim3((unsigned)groups), dim3(64 * kWaves), 0, stream, p, act, (int32_t)j_tiles);
+  hipLaunchKernelGGL((k_moe_few<T, kGated, kFM, kFN, O>), dim3((unsigned)groups), dim3(64 * kWaves), 0, stream, p, act, (int32_t)j_tiles);
   SPTIR_HIP(hipGetLastError());
   return SPTIR_OK;
 }
 
-}  // namespace
-
-sptir_status_t moe_few_forward(int32_t type, int32_t act, const MoeProduct& p, int32_t fragments, hipStream_t stream) {
+template <bool kInt8>
+sptir_status_t launch_few(int32_t type, int32_t act, const MoeProduct& p, int32_t fragments, hipStream_t stream) {
   sptir_status_t st = SPTIR_OK;
   moe_with_type(type, [&](auto v) {
-    using T = decltype(v);
+    using O = decltype(v);
+    using T = std::conditional_t<kInt8, int8_t, O>;
     auto rows = [&](auto fm) {
       constexpr int kFM = decltype(fm)::value;
-      if (act == SPTIR_ACT_SWIGLU) st = launch<T, true, kFM, 2>(act, p, stream);
-      else st = launch<T, false, kFM, kFM == 1 ? 1 : 2>(act, p, stream);
+      if (act == SPTIR_ACT_SWIGLU) st = launch<T, true, kFM, 2, O>(act, p, stream);
+      else st = launch<T, false, kFM, kFM == 1 ? 1 : 2, O>(act, p, stream);
     };
     if (fragments == 1) rows(std::integral_constant<int, 1>{});
     else if (fragments == 2) rows(std::integral_constant<int, 2>{});
     else rows(std::integral_constant<int, 4>{});
   });
   return st;
+}
+
+}  // namespace
+
+sptir_status_t moe_few_forward(int32_t type, int32_t act, const MoeProduct& p, int32_t fragments, hipStream_t stream) {
+  return launch_few<false>(type, act, p, fragments, stream);
+}
+sptir_status_t moe_few_int8(int32_t type, int32_t act, const MoeProduct& p, int32_t fragments, hipStream_t stream) {
+  return launch_few<true>(type, act, p, fragments, stream);
 }
 
 }  // namespace sptir

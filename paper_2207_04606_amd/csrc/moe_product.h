@@ -38,6 +38,11 @@ struct MoeProduct {
   void* db;                   // dw: sums of dZ over an expert's rows; may be NULL
   int64_t db_stride;
   int32_t parts;              // dw: an expert's rows are taken in so many (more than 1: C and db are the workspace's)
+  const float* a_scales;      // 8-bit integers (forward): of x's rows ...
+  const float* b_scales;      // ... and of W's
+  int64_t b_scales_stride;
+  const uint8_t* exponents;   // dx: those of pre, where it is kept in 8 bits
+  int64_t ld_exponents;
 };
 
 // The rows of an m-tile: tiles of `rows` rows, an expert's last one ragged; the rows behind the last expert's are a group of
@@ -61,6 +66,8 @@ inline void moe_divide_by(int32_t k, uint32_t* mul, uint32_t* shift) {
 
 // ------------------------------------------------------------------- matrix instructions
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef int8_t i8x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
@@ -70,21 +77,34 @@ template <typename T>
 struct Mma;
 template <>
 struct Mma<__bf16> {
+  using Acc = f32x4;
   using Frag = bf16x8;
   static __device__ inline f32x4 run(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <>
 struct Mma<_Float16> {
+  using Acc = f32x4;
   using Frag = f16x8;
   static __device__ inline f32x4 run(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 template <>
 struct Mma<float> {
+  using Acc = f32x4;
   using Frag = f32x4;
   static __device__ inline f32x4 run(Frag a, Frag b, f32x4 c) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
     return c;
+  }
+};
+// (sums of at most 131,071 products of two numbers of -128 .. 127 stay below 2^31)
+constexpr int32_t kMoeMostInt8 = 131071;
+template <>
+struct Mma<int8_t> {
+  using Acc = i32x4;
+  using Frag = i8x16;
+  static __device__ inline i32x4 run(Frag a, Frag b, i32x4 c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
   }
 };
 

@@ -2,7 +2,7 @@
 // and the entries sorted by expert.
 #include <algorithm>
 
-#include "moe.h"
+#include "moe_lanes.h"
 
 namespace sptir {
 
@@ -21,47 +21,6 @@ sptir_status_t moe_check_routing(const sptir_moe_routing_t* r) {
 }
 
 namespace {
-
-// A row of 16 lanes turned by n, without a stop in LDS
-template <int kTurn>
-__device__ inline float turned(float v) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + kTurn, 0xf, 0xf, false));
-}
-// over the L = 16 or 64 lanes of a token
-template <int L, typename F>
-__device__ inline float over_lanes(float v, F&& f) {
-  v = f(v, turned<8>(v));
-  v = f(v, turned<4>(v));
-  v = f(v, turned<2>(v));
-  v = f(v, turned<1>(v));
-  if constexpr (L == 64) {
-    v = f(v, __shfl_xor(v, 16));
-    v = f(v, __shfl_xor(v, 32));
-  }
-  return v;
-}
-template <int L>
-__device__ inline float lanes_max(float v) {
-  return over_lanes<L>(v, [](float a, float b) { return fmaxf(a, b); });
-}
-template <int L>
-__device__ inline float lanes_sum(float v) {
-  return over_lanes<L>(v, [](float a, float b) { return a + b; });
-}
-
-// The logits l * C .. l * C + C - 1 of a token's lane l; -inf past the last.
-template <typename T, int C>
-__device__ inline void read_logits(const T* row, int first, int n_experts, float (&l)[C]) {
-  if (first + C <= n_experts) {  // (any alignment of an element)
-    T v[C];
-    __builtin_memcpy(v, row + first, sizeof(v));
-#pragma unroll
-    for (int c = 0; c < C; ++c) l[c] = to_float(v[c]);
-  } else {
-#pragma unroll
-    for (int c = 0; c < C; ++c) l[c] = first + c < n_experts ? to_float(row[first + c]) : -INFINITY;
-  }
-}
 
 // L lanes per token; lane l has the experts l * C .. l * C + C - 1, so that the lowest lane with the largest logit has the
 // lowest id.  Bound by launch and memory latency: k rounds of C comparisons and four turns of 16 lanes, for four tokens of a
@@ -162,47 +121,7 @@ __global__ __launch_bounds__(256) void k_moe_route_backward(const T* __restrict_
     for (int c = 0; c < C; ++c)
       if (e == lane * C + c) d[c] = g;
   }
-  T* out = d_logits + (int64_t)t * ld_d + lane * C;
-  if (lane * C + C <= n_experts) {
-    T v[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) v[c] = from_float<T>(d[c]);
-    __builtin_memcpy(out, v, sizeof(v));
-  } else {
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (lane * C + c < n_experts) out[c] = from_float<T>(d[c]);
-  }
-}
-
-// 16 lanes per token where its experts and choices fit them
-template <typename F>
-void with_lanes(int32_t n_experts, int32_t top_k, F&& f) {
-  using std::integral_constant;
-  if (top_k <= 16 && n_experts <= 256) {
-    const integral_constant<int, 16> lanes;
-    if (n_experts <= 16) f(lanes, integral_constant<int, 1>{});
-    else if (n_experts <= 32) f(lanes, integral_constant<int, 2>{});
-    else if (n_experts <= 64) f(lanes, integral_constant<int, 4>{});
-    else if (n_experts <= 128) f(lanes, integral_constant<int, 8>{});
-    else f(lanes, integral_constant<int, 16>{});
-  } else {
-    const integral_constant<int, 64> lanes;
-    if (n_experts <= 256) f(lanes, integral_constant<int, 4>{});
-    else if (n_experts <= 512) f(lanes, integral_constant<int, 8>{});
-    else f(lanes, integral_constant<int, 16>{});
-  }
-}
-
-// f(first token, tokens, grid) for as many launches as it takes: one of 2^32 threads and more runs only what is over, and says nothing.
-constexpr int32_t kLaunchTokens = 1 << 25;  // (2^31 threads with 64 lanes a token)
-template <typename F>
-void in_launches(int32_t n_tokens, int lanes, F&& f) {
-  const int32_t each = 256 / lanes;  // of a workgroup
-  for (int64_t t = 0; t < n_tokens; t += kLaunchTokens) {
-    const int32_t n = (int32_t)std::min<int64_t>(n_tokens - t, kLaunchTokens);
-    f(t, n, dim3((unsigned)((n + each - 1) / each)));
-  }
+  write_logits<T, C>(d_logits + (int64_t)t * ld_d, lane * C, n_experts, d);
 }
 
 // ------------------------------------------------------------------- sort by expert

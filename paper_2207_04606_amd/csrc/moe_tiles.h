@@ -2,6 +2,7 @@
 #ifndef SPTIR_MOE_TILES_H_
 #define SPTIR_MOE_TILES_H_
 
+#include "moe_codes.h"
 #include "moe_product.h"
 
 namespace sptir {
@@ -139,6 +140,18 @@ __device__ inline void write_8(T* p, int32_t many, const float (&v)[8]) {
     }
   }
 }
+// ... of a row that is kept in 8 bits, from column j on (kOne: all in one block): as T they are what they stand for, exactly
+template <typename T, bool kOne>
+__device__ inline Eight<T> kept_8(const int8_t* codes, const uint8_t* exponents, int64_t j, int32_t many) {
+  constexpr int kN = Eight<T>::kN;
+  Eight<T> e = {};
+  if (many <= 0) return e;
+  float v[8];
+  read_kept<8, kOne>(codes, exponents, j, many, v);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) e.w[i / kN][i % kN] = from_float<T>(v[i]);
+  return e;
+}
 template <int kAct, typename T>
 __device__ inline void act_8(float (&v)[8]) {
 #pragma unroll
@@ -231,14 +244,16 @@ __device__ inline void moe_clear_8(const MoeProduct& p, int64_t i, int32_t j, in
 
 constexpr int kMoeStep = 64;  // most of r that a step takes
 // the tiles' kernels count 16-byte words of an operand (of a step's lines, where they lie across) with 32 bits
-inline bool moe_near(int32_t type, int64_t rows, int64_t ld) {
-  return rows == 0 || ld < ((int64_t)1 << 32) * (16 / moe_type_bytes(type)) / rows;
-}
+inline bool moe_near_elements(int in_word, int64_t rows, int64_t ld) { return rows == 0 || ld < ((int64_t)1 << 32) * in_word / rows; }
+inline bool moe_near(int32_t type, int64_t rows, int64_t ld) { return moe_near_elements(16 / moe_type_bytes(type), rows, ld); }
 
 // ---- launches (moe_few.hip, moe_tiles_*.hip; words: in 16-byte words throughout)
 sptir_status_t moe_few_forward(int32_t type, int32_t act, const MoeProduct& p, int32_t fragments, hipStream_t stream);
 sptir_status_t moe_tiles_forward(int32_t type, int32_t act, bool words, bool wide, const MoeProduct& p, hipStream_t stream);
 sptir_status_t moe_tiles_dx(int32_t type, int32_t act, bool words, bool wide, const MoeProduct& p, hipStream_t stream);
+sptir_status_t moe_few_int8(int32_t type, int32_t act, const MoeProduct& p, int32_t fragments, hipStream_t stream);
+sptir_status_t moe_tiles_int8(int32_t type, int32_t act, bool words, bool wide, const MoeProduct& p, hipStream_t stream);
+sptir_status_t moe_tiles_dx_kept(int32_t type, int32_t act, bool words, bool wide, const MoeProduct& p, hipStream_t stream);
 sptir_status_t moe_tiles_dw(int32_t type, bool words, const MoeProduct& p, void* workspace, hipStream_t stream);
 
 }  // namespace sptir

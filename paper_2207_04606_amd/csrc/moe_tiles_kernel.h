@@ -95,7 +95,11 @@ __device__ inline void loads_arrived() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 // kWords: the operands, and what the epilogue reads and writes, lie in 16-byte words: chunks go from memory to LDS by
 // themselves, and their places are counted in words with 32 bits.  Otherwise a thread reads them from where they are and
 // writes them to LDS a step later.
-template <typename T, MoeOp kOp, MoeEnd kEnd, bool kWords, typename S>
+//
+// T: the operands' type, O that of everything else.  T of 8-bit integers (forward): the sums are whole numbers, of 128 r a step, and z is
+// (sum * the scale of x's row) * the scale of W's row.  A tile's scales, a float of each thread, go to LDS with its first loads.
+// kKept (dx): pre is kept in 8 bits.
+template <typename T, MoeOp kOp, MoeEnd kEnd, bool kWords, typename S, typename O = T, bool kKept = false>
 __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(MoeProduct p, int32_t act, int32_t j_tiles, int32_t i_tiles) {
   extern __shared__ __attribute__((aligned(16))) char lds_generic[];
   lds_char* lds = (lds_char*)lds_generic;
@@ -105,6 +109,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   constexpr bool kGated = kOp == kMoeForward && kEnd == kEndSwiglu;  // (C has half the columns)
   constexpr int kColsC = kGated ? S::kBN / 2 : S::kBN;
   static_assert(k16 || kAAlongR || S::kFM == 4, "rows of float32 lines across are taken by four");
+  constexpr bool kInt8 = std::is_same_v<T, int8_t>;
+  static_assert(!kInt8 || (kOp == kMoeForward && kThreads == S::kBM + S::kBN), "a scale of each thread");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t out_cols = kGated ? p.n_j / 2 : p.n_j;
 
@@ -117,8 +123,10 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
 
   // ---- the tiles of this workgroup
   const uint32_t per_expert = (uint32_t)i_tiles * j_tiles;
-  const MoeTable table = {(int32_t*)(lds_generic + 2 * S::kStage), (int32_t*)(lds_generic + 2 * S::kStage) + p.n_experts + 2};
-  const int32_t* order = kOp == kMoeDw ? moe_rank_experts(p, (int32_t*)(lds_generic + 2 * S::kStage)) : nullptr;
+  constexpr int kScales = kInt8 ? kThreads * (int)sizeof(float) : 0;  // (of the tile that is worked on and of the next)
+  int32_t* const behind = (int32_t*)(lds_generic + 2 * S::kStage + 2 * kScales);
+  const MoeTable table = {behind, behind + p.n_experts + 2};
+  const int32_t* order = kOp == kMoeDw ? moe_rank_experts(p, behind) : nullptr;
   const uint32_t m_tiles = kOp == kMoeDw ? 0 : moe_fill_table(p, S::kBM, table);
   const uint32_t total = kOp == kMoeDw ? per_expert * p.n_experts * (kEnd >= kEndParts ? p.parts : 1) : m_tiles * j_tiles;
   MoeTile t;
@@ -134,11 +142,11 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   auto chunk_a = [&](int n) { return tid % kLineA ^ (kAAlongR ? key_rows(a_line(n)) : k16 ? key_tr_rows(a_line(n)) : 0); };
   auto chunk_b = [&](int n) { return tid % kLineB ^ (kBAlongR ? key_cols(b_line(n)) : k16 ? key_tr_cols(b_line(n)) : 0); };
   auto a_row = [&](int n) { return min(t.first + a_line(n), t.end - 1); };  // lines along r: the sorted row
-  auto b_row = [&](int n) {  // (forward) the row of W[e]; gated: of 16 lines 8 gates, then the 8 that go with them
-    const int line = b_line(n);
+  auto w_row = [&](int line) {  // (forward) the row of W[e]; gated: of 16 lines 8 gates, then the 8 that go with them
     if (kGated) return min(j0 + line / 16 * 8 + line % 8, out_cols - 1) + (line & 8 ? out_cols : 0);
     return min(j0 + line, p.n_j - 1);
   };
+  auto b_row = [&](int n) { return w_row(b_line(n)); };
   // kWords: places in units of 16 bytes from the step's base on.  Otherwise addresses, and what was read for a later step.
   constexpr int kPlaces = kWords ? kLoads : 1, kHeld = kWords ? 1 : kLoads;
   uint32_t place[kPlaces];
@@ -150,6 +158,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   constexpr bool kParts = kEnd == kEndParts || kEnd == kEndPartsSum;  // (dw: sums of parts of an expert's rows, in float32)
   constexpr bool kSumZ = kOp == kMoeDw && (kEnd == kEndAct || kEnd == kEndPartsSum);  // (db is asked for)
   bool sum_z = false;  // this tile's workgroup sums dZ too
+  int scales_at = 1;   // (8-bit integers) which of the two places has this tile's scales
   auto start = [&](uint32_t id) __attribute__((always_inline)) {
     uint32_t dealt = moe_deal(id, total);
     int jt;
@@ -193,6 +202,22 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
         int32_t entry[kLoadsA];
         each<kLoadsA>([&](auto n) { entry[n] = p.entry_of[rows[n]]; });
         each<kLoadsA>([&](auto n) { rows[n] = moe_token(p, entry[n]); });
+      }
+    }
+    if constexpr (kInt8) {
+      if (steps > 0) {
+        const float* at;
+        if (tid < S::kBM) {
+          int64_t row = min(t.first + tid, t.end - 1);
+          if (p.entry_of) row = moe_token(p, p.entry_of[row]);
+          at = p.a_scales + row;
+        } else {
+          at = p.b_scales + t.expert * p.b_scales_stride + w_row(tid - S::kBM);
+        }
+        // (Whoever read this place before did so ahead of the barriers of the tile in between: only tiles that have steps change places.)
+        scales_at ^= 1;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)at,
+                                         (__attribute__((address_space(3))) void*)(lds + 2 * S::kStage + scales_at * kScales + wave * 256), 4, 0, 0);
       }
     }
     each<kLoadsA>([&](auto n) {
@@ -291,7 +316,9 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   using M = Mma<T>;
   using Frag = typename M::Frag;
   constexpr int kZ = S::kFM / S::kWavesN;  // fragments of rows whose sums of dZ a wavefront has
-  f32x4 acc[S::kFM][S::kFN], acc_z[kSumZ ? kZ : 1];
+  using Acc = typename M::Acc;
+  Acc acc[S::kFM][S::kFN];
+  f32x4 acc_z[kSumZ ? kZ : 1];
   // A phase multiplies two fragments of rows with the columns', 64 bytes of r, while the fragments of the next phase are read.
   constexpr int kPhases = S::kFM / 2, kHalves = 2;
   static_assert(kPhases % 2 == 0, "the sets of fragments alternate");
@@ -419,7 +446,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   start(id);
   load_first();
   while (true) {
-    each<S::kFM>([&](auto f) { each<S::kFN>([&](auto g) { acc[f][g] = f32x4{0.f, 0.f, 0.f, 0.f}; }); });
+    each<S::kFM>([&](auto f) { each<S::kFN>([&](auto g) { acc[f][g] = Acc{}; }); });
     if (kSumZ) each<kZ>([&](auto f) { acc_z[kSumZ ? (int)f : 0] = f32x4{0.f, 0.f, 0.f, 0.f}; });
     if (steps > 0) {
       if constexpr (!kWords) {
@@ -444,6 +471,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
     const MoeTile done = t;
     const int32_t done_j0 = j0;
     const bool done_sum_z = sum_z;
+    const int done_steps = steps, done_scales = scales_at;
     id += gridDim.x;
     const bool more = id < total;
     if (more) {
@@ -460,32 +488,40 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
     const int my_row = wi + (my_lane & 15) * (k16 || kAAlongR ? 1 : 4), my_q = my_lane >> 4;
     const bool none = kOp != kMoeDw && done.expert == p.n_experts;
     const int32_t my_j = done_j0 + (kGated ? wj / 2 + my_q * 8 : wj + my_q * 16);
-    const T* other_at = (const T*)(kOp == kMoeForward ? p.residual : p.pre);
+    const O* other_at = (const O*)(kOp == kMoeForward ? p.residual : p.pre);
     const int64_t other_ld = kOp == kMoeForward ? p.ld_residual : p.ld_pre;
     if (none) {
       for (int f = 0; f < S::kFM; ++f) {
         const int64_t i = done.first + my_row + kRowApart * f;
         each<kGated ? 1 : 2>([&](auto x) {
           const int32_t j = my_j + x * 8;
-          if (i < done.end && j < out_cols) moe_clear_8<T, kOp, kEnd, kWords>(p, i, j, out_cols - j);
+          if (i < done.end && j < out_cols) moe_clear_8<O, kOp, kEnd, kWords>(p, i, j, out_cols - j);
         });
       }
     } else {
       const bool other_too = kOp == kMoeForward ? p.residual != nullptr : kOp == kMoeDx && kEnd != kEndNone;
-      Eight<T> bias[2] = {}, other[2][2] = {}, pair[2][2] = {};  // (what there is none of adds zeros)
+      Eight<O> bias[2] = {}, other[2][2] = {}, pair[2][2] = {};  // (what there is none of adds zeros)
       constexpr int kAtOnce = kOp == kMoeDx && kEnd == kEndSwiglu ? 1 : 2;  // (what is read is twice as much there)
       each<S::kFM / kAtOnce>([&](auto fs) {
         if (kOp == kMoeForward && p.bias) {
-          const T* at = (const T*)p.bias + done.expert * p.bias_stride + my_j;
-          each<2>([&](auto x) { bias[x] = read_8<T, kWords>(at + (kGated ? x * out_cols : x * 8), out_cols - my_j - (kGated ? 0 : x * 8)); });
+          const O* at = (const O*)p.bias + done.expert * p.bias_stride + my_j;
+          each<2>([&](auto x) { bias[x] = read_8<O, kWords>(at + (kGated ? x * out_cols : x * 8), out_cols - my_j - (kGated ? 0 : x * 8)); });
           loads_arrived();
         }
         if (other_too) {
           each<kAtOnce>([&](auto f) {
-            const T* at = other_at + min(done.first + my_row + kRowApart * (fs * kAtOnce + f), done.end - 1) * other_ld + my_j;
+            const int64_t i = min(done.first + my_row + kRowApart * (fs * kAtOnce + f), done.end - 1);
+            [[maybe_unused]] const O* at = other_at + i * other_ld + my_j;
             each<kGated ? 1 : 2>([&](auto x) {
-              other[f][x] = read_8<T, kWords>(at + x * 8, out_cols - my_j - x * 8);
-              if constexpr (kOp == kMoeDx && kEnd == kEndSwiglu) pair[f][x] = read_8<T, kWords>(at + x * 8 + p.n_j, out_cols - my_j - x * 8);
+              if constexpr (kKept) {
+                const int8_t* codes = (const int8_t*)p.pre + i * other_ld;
+                const uint8_t* exponents = p.exponents + i * p.ld_exponents;
+                other[f][x] = kept_8<O, true>(codes, exponents, my_j + x * 8, out_cols - my_j - x * 8);
+                if constexpr (kEnd == kEndSwiglu) pair[f][x] = kept_8<O, kWords && sizeof(O) == 2>(codes, exponents, (int64_t)my_j + x * 8 + p.n_j, out_cols - my_j - x * 8);
+              } else {
+                other[f][x] = read_8<O, kWords>(at + x * 8, out_cols - my_j - x * 8);
+                if constexpr (kOp == kMoeDx && kEnd == kEndSwiglu) pair[f][x] = read_8<O, kWords>(at + x * 8 + p.n_j, out_cols - my_j - x * 8);
+              }
             });
           });
           loads_arrived();
@@ -498,17 +534,25 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
           // (float32 columns across: the four of a lane are those of its four fragments)
           each<16>([&](auto nth) {
             constexpr int x = decltype(nth)::value;
-            v[x] = k16 || kBAlongR ? acc[f][x / 4][x % 4] : acc[f][x % 4][x / 4];
+            v[x] = (float)(k16 || kBAlongR ? acc[f][x / 4][x % 4] : acc[f][x % 4][x / 4]);
           });
+          if constexpr (kInt8) {
+            typedef __attribute__((address_space(3))) const float lds_float;
+            lds_float* scales = (lds_float*)(lds + 2 * S::kStage + done_scales * kScales);
+            if (done_steps > 0) {  // (otherwise there are none, and the sums are zeros)
+              const float mine = scales[my_row + 16 * f];
+              each<16>([&](auto x) { v[x] = v[x] * mine * scales[S::kBM + wj + my_q * 16 + x]; });
+            }
+          }
           if (i >= done.end) return;
           if constexpr (kGated) {
             if (my_j >= out_cols) return;
-            moe_emit_gated_8<T, kWords>(p, i, my_j, out_cols - my_j, v, v + 8, bias[0], bias[1], other[ff][0]);
+            moe_emit_gated_8<O, kWords>(p, i, my_j, out_cols - my_j, v, v + 8, bias[0], bias[1], other[ff][0]);
           } else {
             each<2>([&](auto x) {
               const int32_t j = my_j + x * 8;
               if (j >= out_cols) return;
-              moe_emit_8<T, kOp, kEnd, kWords>(p, act, done.expert, i, j, out_cols - j, v + x * 8, bias[x], other[ff][x], pair[ff][x]);
+              moe_emit_8<O, kOp, kEnd, kWords>(p, act, done.expert, i, j, out_cols - j, v + x * 8, bias[x], other[ff][x], pair[ff][x]);
             });
           }
         });
@@ -533,7 +577,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
 using Wide = Shape<kMoeWide.rows, kMoeWide.cols, 2, 4, kMoeWide.groups>;
 using Narrow = Shape<kMoeNarrow.rows, kMoeNarrow.cols, 2, 2, kMoeNarrow.groups>;
 
-template <MoeOp kOp, bool kWords, typename S>
+template <MoeOp kOp, bool kWords, typename S, bool kInt8 = false, bool kKept = false>
 sptir_status_t launch(int32_t type, int32_t act, const MoeProduct& p, int32_t out_cols, int32_t cols, hipStream_t stream) {
   const int64_t j_tiles = std::max((out_cols + cols - 1) / cols, kOp == kMoeDw && p.db ? 1 : 0);  // (db is summed beside dW's first columns)
   const int64_t i_tiles = kOp == kMoeDw ? (p.n_i + S::kBM - 1) / S::kBM : moe_most_tiles(p.n_rows, p.n_experts, p.expert_ptr, S::kBM);
@@ -542,9 +586,10 @@ sptir_status_t launch(int32_t type, int32_t act, const MoeProduct& p, int32_t ou
   if (tiles > (int64_t)INT32_MAX) return SPTIR_ERR_OVERFLOW;
   const int64_t groups = std::min<int64_t>(tiles, (int64_t)256 * S::kGroups);  // those that run at once
   auto go = [&](auto v, auto end) {
-    auto* kernel = k_moe_tiles<decltype(v), kOp, decltype(end)::value, kWords, S>;
+    using O = decltype(v);
+    auto* kernel = k_moe_tiles<std::conditional_t<kInt8, int8_t, O>, kOp, decltype(end)::value, kWords, S, O, kKept>;
     static OncePerDevice allowed;
-    const int lds = 2 * S::kStage + (kOp == kMoeDw ? moe_ranks_bytes(p) : moe_table_bytes(p.expert_ptr, p.n_experts));
+    const int lds = 2 * S::kStage + (kInt8 ? 2 * S::kThreads * (int)sizeof(float) : 0) + (kOp == kMoeDw ? moe_ranks_bytes(p) : moe_table_bytes(p.expert_ptr, p.n_experts));
     allow_dynamic_lds((const void*)kernel, lds, allowed);
     hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(S::kThreads), lds, stream, p, act, (int32_t)j_tiles, (int32_t)i_tiles);
   };
@@ -561,11 +606,11 @@ sptir_status_t launch(int32_t type, int32_t act, const MoeProduct& p, int32_t ou
     } else if (p.db) {
       return go(v, std::integral_constant<MoeEnd, kEndAct>{});
     }
-    go(v, std::integral_constant<MoeEnd, kEndNone>{});
+    if constexpr (!kKept) go(v, std::integral_constant<MoeEnd, kEndNone>{});
   };
   if (type == SPTIR_F16) with(_Float16{});
   else if (type == SPTIR_BF16) with(__bf16{});
-  else if constexpr (S::kBM <= 128) with(float{});
+  else if constexpr (S::kBM <= 128 || kInt8) with(float{});
   SPTIR_HIP(hipGetLastError());
   return SPTIR_OK;
 }
@@ -576,12 +621,12 @@ int32_t columns(int32_t act) { return kOp == kMoeForward && act == SPTIR_ACT_SWI
 template <MoeOp kOp>
 int32_t columns(int32_t act, const MoeProduct& p) { return kOp == kMoeForward && act == SPTIR_ACT_SWIGLU ? p.n_j / 2 : p.n_j; }
 
-template <MoeOp kOp>
+template <MoeOp kOp, bool kInt8 = false, bool kKept = false>
 sptir_status_t launch_tiles(int32_t type, int32_t act, bool words, bool wide, const MoeProduct& p, hipStream_t stream) {
   const int32_t out_cols = columns<kOp>(act, p);
-  if (!words) return launch<kOp, false, Narrow>(type, act, p, out_cols, columns<kOp, Narrow>(act), stream);
-  if (wide) return launch<kOp, true, Wide>(type, act, p, out_cols, columns<kOp, Wide>(act), stream);
-  return launch<kOp, true, Narrow>(type, act, p, out_cols, columns<kOp, Narrow>(act), stream);
+  if (!words) return launch<kOp, false, Narrow, kInt8, kKept>(type, act, p, out_cols, columns<kOp, Narrow>(act), stream);
+  if (wide) return launch<kOp, true, Wide, kInt8, kKept>(type, act, p, out_cols, columns<kOp, Wide>(act), stream);
+  return launch<kOp, true, Narrow, kInt8, kKept>(type, act, p, out_cols, columns<kOp, Narrow>(act), stream);
 }
 
 }  // namespace
