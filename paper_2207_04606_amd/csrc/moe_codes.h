@@ -34,17 +34,24 @@ __device__ inline Codes<kN> read_codes(const int8_t* p, int many) {
   return c;
 }
 
-// kN values of a row from column c on, `many` of which are there.  They may lie in two blocks (kOne: they do not).
+// kN elements of a row from column c on, `many` of which are there (one at least).  They may lie in two blocks (kOne: they do not).
 template <int kN, bool kOne>
-__device__ inline void read_kept(const int8_t* row, const uint8_t* exponents, int64_t c, int many, float (&v)[kN]) {
-  const Codes<kN> codes = read_codes<kN>(row + c, many);
-  const float unit = code_unit(exponents[c / kMoeBlock]);
-  float next = unit;
-  if (!kOne && many > 0) next = code_unit(exponents[(c + (many < kN ? many : kN) - 1) / kMoeBlock]);
-  const int over = kMoeBlock - (int)(c % kMoeBlock);  // the first of the next block
+struct Kept {
+  Codes<kN> codes;
+  uint32_t first, next;  // exponents
+  int over;              // the first element of the next block
+  __device__ inline void read(const int8_t* row, const uint8_t* exponents, int64_t c, int many) {
+    codes = read_codes<kN>(row + c, many);
+    first = next = exponents[c / kMoeBlock];
+    if (!kOne) next = exponents[(c + (many < kN ? many : kN) - 1) / kMoeBlock];
+    over = kMoeBlock - (int)(c % kMoeBlock);
+  }
+  __device__ inline void values(float (&v)[kN]) const {
+    const float unit = code_unit(first), other = kOne ? unit : code_unit(next);
 #pragma unroll
-  for (int i = 0; i < kN; ++i) v[i] = codes.at(i) * (kOne || i < over ? unit : next);
-}
+    for (int i = 0; i < kN; ++i) v[i] = codes.at(i) * (kOne || i < over ? unit : other);
+  }
+};
 
 // (moe_rows8.hip) sptir_moe_unpack, its arguments checked
 sptir_status_t moe_unpack(int32_t type, int32_t act, int32_t width, int64_t n_rows, const int8_t* Q, int64_t ldq, const uint8_t* exponents,

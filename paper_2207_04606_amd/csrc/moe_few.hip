@@ -150,6 +150,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_moe_few(MoeProduct p, int32_t a
     int64_t r = wave * kStep;
     for (; r + (kTurns - 1) * kWaves * kStep + kStep <= p.n_r; r += kTurns * kWaves * kStep)
       turns(r, std::integral_constant<int, kTurns>{}, std::true_type{});
+    if (kTurns > 2)  // (of 2048 8-bit integers or 1024 of 16 bits a wavefront has two turns: 8 experts' 2048 x 2048 bytes for one token 10.4 -> 8.9 us)
+      for (; r + kWaves * kStep + kStep <= p.n_r; r += 2 * kWaves * kStep) turns(r, std::integral_constant<int, 2>{}, std::true_type{});
     if (kTurns > 1)
       for (; r + kStep <= p.n_r; r += kWaves * kStep) turns(r, std::integral_constant<int, 1>{}, std::true_type{});
     if (r < p.n_r) turns(r, std::integral_constant<int, 1>{}, std::false_type{});

@@ -58,15 +58,16 @@ __device__ inline void read_logits(const T* row, int first, int n_experts, float
 }
 template <typename T, int C>
 __device__ inline void write_logits(T* row, int first, int n_experts, const float (&d)[C]) {
+  T* out = row + first;
   if (first + C <= n_experts) {
     T v[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) v[c] = from_float<T>(d[c]);
-    __builtin_memcpy(row + first, v, sizeof(v));
+    __builtin_memcpy(out, v, sizeof(v));
   } else {
 #pragma unroll
     for (int c = 0; c < C; ++c)
-      if (first + c < n_experts) row[first + c] = from_float<T>(d[c]);
+      if (first + c < n_experts) out[c] = from_float<T>(d[c]);
   }
 }
 

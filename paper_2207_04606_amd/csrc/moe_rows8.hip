@@ -11,7 +11,7 @@ namespace {
 struct Rows8 {
   int64_t n_rows;
   int32_t width;
-  int32_t lanes;  // of a row: a power of two from 8 to 64, or 256
+  int32_t lanes, shift;  // of a row: 2^shift from 8 to 64, or 256
   const void* X;  // quantise, pack
   int64_t ldx;
   int8_t* Q;
@@ -25,33 +25,37 @@ struct Rows8 {
   uint32_t top;   // ... and the one with which 64 is past the type's range
 };
 
-// The first `many` elements of a word of T, as floats, zeros behind them
+// The first `many` elements of a 16-byte word of T, zeros behind them
 template <typename T>
 struct Word {
   static constexpr int kN = 16 / sizeof(T);
-  float v[kN];
+  u32x4 w;
+  __device__ inline float at(int i) const {
+    if constexpr (sizeof(T) == 4) {
+      const uint32_t bits = w[i];  // (a bit_cast of an element of a vector takes the first one)
+      return __builtin_bit_cast(float, bits);
+    } else {
+      const uint16_t bits = (uint16_t)(w[i / 2] >> i % 2 * 16);
+      return to_float(__builtin_bit_cast(T, bits));
+    }
+  }
 };
 template <typename T>
 __device__ inline Word<T> read_word(const T* p, int many) {
-  constexpr int kN = Word<T>::kN;
   Word<T> w;
-  T e[kN];
-  if (many >= kN) {
-    __builtin_memcpy(e, p, 16);
-  } else {
-#pragma unroll
-    for (int i = 0; i < kN; ++i) e[i] = i < many ? p[i] : from_float<T>(0.f);
-  }
-#pragma unroll
-  for (int i = 0; i < kN; ++i) w.v[i] = to_float(e[i]);
+  if (many >= Word<T>::kN) __builtin_memcpy(&w.w, p, 16);
+  else w.w = read_elements(p, max(many, 0));
   return w;
 }
+// The low bytes of kN numbers
 template <int kN>
-__device__ inline void write_codes(int8_t* p, int many, const int (&q)[kN]) {
+__device__ inline void write_codes(int8_t* p, int many, const uint32_t (&q)[kN]) {
   uint32_t w[kN / 4];
 #pragma unroll
-  for (int i = 0; i < kN / 4; ++i)
-    w[i] = (q[4 * i] & 255) | (q[4 * i + 1] & 255) << 8 | (q[4 * i + 2] & 255) << 16 | (uint32_t)q[4 * i + 3] << 24;
+  for (int i = 0; i < kN / 4; ++i) {
+    const uint32_t lo = __builtin_amdgcn_perm(q[4 * i + 1], q[4 * i], 0x0c0c0400), hi = __builtin_amdgcn_perm(q[4 * i + 3], q[4 * i + 2], 0x0c0c0400);
+    w[i] = hi << 16 | lo;
+  }
   if (many >= kN) {
     __builtin_memcpy(p, w, kN);
   } else {
@@ -61,14 +65,30 @@ __device__ inline void write_codes(int8_t* p, int many, const int (&q)[kN]) {
   }
 }
 
-// The largest magnitude, as its bits: those of infinities and NaN are above all others'.
+// The largest magnitude, as the bits of a T without their sign: those of infinities and NaN are above all others'.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 template <typename T>
-__device__ inline uint32_t largest(const Word<T>& w) {
-  uint32_t m = 0;
+struct Largest {
+  uint32_t m = 0;  // (16 bits: of the even and of the odd elements)
+  __device__ inline void take(uint32_t bits) {
+    if constexpr (sizeof(T) == 4) m = max(m, bits);
+    else m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m), __builtin_bit_cast(u16x2, bits)));
+  }
+  __device__ inline void take(const Word<T>& w) {
 #pragma unroll
-  for (int i = 0; i < Word<T>::kN; ++i) m = max(m, __builtin_bit_cast(uint32_t, w.v[i]) & 0x7fffffffu);
-  return m;
-}
+    for (int i = 0; i < 4; ++i) take(w.w[i] & (sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu));
+  }
+  // as a float32
+  __device__ inline float value() const {
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, m);
+    else return to_float(__builtin_bit_cast(T, (uint16_t)max(m & 0xffff, m >> 16)));
+  }
+};
+template <int kTurn>
+__device__ inline uint32_t turned_bits(uint32_t v) { return __builtin_amdgcn_update_dpp(0, (int)v, 0x120 + kTurn, 0xf, 0xf, false); }
+
+// Rounding by an addition: 1.5 * 2^23 + a number below 2^22 is rounded to a whole number, to even, whose two's complement has the low bits.
+constexpr float kRound = 12582912.f;
 
 // The whole number nearest to x / s, the even one of two: a guess, one off at most, and what it leaves, which is exact.  (With u the unit of s's
 // last place, x and the guess times s are multiples of u / 2; what is left, up to s / 2, is below 2^24 of them, and where it is more
@@ -84,40 +104,66 @@ __device__ inline int nearest(float x, float s, float inverse) {
 
 constexpr int kHeldWords = 4;  // of a row, that a lane keeps between the maximum and the codes
 
-// A group of lanes per row: the largest magnitude, then the codes.
+// A group of lanes per row: the largest magnitude, then the codes.  An element's code is x times the reciprocal of the scale, rounded: within 2^-16 of
+// the quotient, so the nearest one wherever that is not next to the middle of two; a word with such a one (of 512 elements 1 in 30) is done with
+// care.
 template <typename T>
 __global__ __launch_bounds__(256) void k_moe_quantise(Rows8 p) {
   constexpr int kN = Word<T>::kN;
   __shared__ uint32_t part[4];
   const int lane = threadIdx.x & (p.lanes - 1);
-  const int64_t groups = (int64_t)gridDim.x * (256 / p.lanes);
+  const int64_t groups = (int64_t)gridDim.x << (8 - p.shift);
   const int apart = p.lanes * kN;
-  for (int64_t r = (int64_t)blockIdx.x * (256 / p.lanes) + threadIdx.x / p.lanes; r < p.n_rows; r += groups) {
+  for (int64_t r = ((int64_t)blockIdx.x << (8 - p.shift)) + (threadIdx.x >> p.shift); r < p.n_rows; r += groups) {
     const T* x = (const T*)p.X + r * p.ldx;
     Word<T> held[kHeldWords];
-    uint32_t m = 0;
+    Largest<T> most;
 #pragma unroll
     for (int h = 0; h < kHeldWords; ++h) held[h] = read_word<T>(x + lane * kN + h * apart, p.width - lane * kN - h * apart);
 #pragma unroll
-    for (int h = 0; h < kHeldWords; ++h) m = max(m, largest<T>(held[h]));
-    for (int c = lane * kN + kHeldWords * apart; c < p.width; c += apart) m = max(m, largest<T>(read_word<T>(x + c, p.width - c)));
-    for (int d = min(p.lanes, 64) / 2; d; d >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
+    for (int h = 0; h < kHeldWords; ++h) most.take(held[h]);
+    for (int c = lane * kN + kHeldWords * apart; c < p.width; c += apart) most.take(read_word<T>(x + c, p.width - c));
+    if (p.lanes >= 16) {
+      most.take(turned_bits<8>(most.m));
+      most.take(turned_bits<4>(most.m));
+      most.take(turned_bits<2>(most.m));
+      most.take(turned_bits<1>(most.m));
+      for (int d = min(p.lanes, 64) / 2; d >= 16; d >>= 1) most.take((uint32_t)__shfl_xor((int)most.m, d));
+    } else {
+      for (int d = 4; d; d >>= 1) most.take((uint32_t)__shfl_xor((int)most.m, d));
+    }
     if (p.lanes > 64) {
-      if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+      if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most.m;
       __syncthreads();
-      m = max(max(part[0], part[1]), max(part[2], part[3]));
+#pragma unroll
+      for (int w = 0; w < 4; ++w) most.take(part[w]);
       __syncthreads();
     }
-    const bool finite = m < 0x7f800000u;
-    const float s = finite ? __builtin_bit_cast(float, m) / 127.f : __builtin_nanf("");
+    const float m = most.value();
+    const bool finite = m < INFINITY;
+    const float s = finite ? m / 127.f : __builtin_nanf("");
     if (lane == 0) p.scales[r] = s;
     // (the reciprocal of a scale near float32's smallest would be infinite; a row of zeros has the scale 0 and the codes 0)
-    const bool some = finite && s > 0.f;
-    const float up = m < 0x21800000u ? 0x1p64f : 1.f, su = s * up, inverse = 1.f / su;
+    const bool small = m < 0x1p-60f;
+    const float up = small ? 0x1p64f : 1.f, su = s * up, inverse = finite && s > 0.f ? 1.f / su : 0.f;
     auto put = [&](const Word<T>& w, int c) {
-      int q[kN];
+      uint32_t q[kN];
+      float near = 0.f;  // how near the middle the nearest to it is
 #pragma unroll
-      for (int i = 0; i < kN; ++i) q[i] = some ? nearest(w.v[i] * up, su, inverse) : 0;
+      for (int i = 0; i < kN; ++i) {
+        const float v = w.at(i), sum = fmaf(v, inverse, kRound);
+        q[i] = __builtin_bit_cast(uint32_t, sum);
+        near = fmaxf(near, fabsf(fmaf(v, inverse, kRound - sum)));
+      }
+      if (!(near < 0.5f - 0x1p-15f) || small || !finite) {
+#pragma unroll 1
+        for (int i = 0; i < kN; ++i) {
+          const int n = inverse > 0.f ? nearest(w.at(i) * up, su, inverse) : 0;
+#pragma unroll
+          for (int o = 0; o < kN; ++o)
+            if (o == i) q[o] = (uint32_t)n;
+        }
+      }
       write_codes<kN>(p.Q + r * p.ldq + c, p.width - c, q);
     };
 #pragma unroll
@@ -134,20 +180,26 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_moe_pack(Rows8 p) {
   constexpr int kN = Word<T>::kN, kLanes = kMoeBlock / kN;
   const int lane = threadIdx.x & (p.lanes - 1);
-  const int64_t groups = (int64_t)gridDim.x * (256 / p.lanes);
+  const int64_t groups = (int64_t)gridDim.x << (8 - p.shift);
   const int padded = (p.width + kMoeBlock - 1) / kMoeBlock * kMoeBlock;  // (a block's lanes stay together)
-  for (int64_t r = (int64_t)blockIdx.x * (256 / p.lanes) + threadIdx.x / p.lanes; r < p.n_rows; r += groups) {
+  for (int64_t r = ((int64_t)blockIdx.x << (8 - p.shift)) + (threadIdx.x >> p.shift); r < p.n_rows; r += groups) {
     for (int c = lane * kN; c < padded; c += p.lanes * kN) {
       const Word<T> w = read_word<T>((const T*)p.X + r * p.ldx + c, p.width - c);
-      uint32_t m = largest<T>(w);
+      Largest<T> most;
+      most.take(w);
 #pragma unroll
-      for (int d = 1; d < kLanes; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
+      for (int d = 1; d < kLanes; d <<= 1) most.take((uint32_t)__shfl_xor((int)most.m, d));
+      const uint32_t m = __builtin_bit_cast(uint32_t, most.value());
       const bool finite = m < 0x7f800000u;
       const uint32_t e = finite ? (uint32_t)max((int)((m + 0x10000u) >> 23) - 6, p.least) : 255u;
-      const float inverse = __builtin_bit_cast(float, (254u - min(e, 253u)) << 23), most = e == p.top ? 63.f : 127.f;
-      int q[kN];
+      const float inverse = __builtin_bit_cast(float, (254u - min(e, 253u)) << 23);
+      uint32_t q[kN];
 #pragma unroll
-      for (int i = 0; i < kN; ++i) q[i] = finite ? (int)fminf(fmaxf(rintf(w.v[i] * inverse), -most), most) : 0;
+      for (int i = 0; i < kN; ++i) q[i] = __builtin_bit_cast(uint32_t, fmaf(w.at(i), inverse, kRound));
+      if (e >= p.top) {  // (or 255: the codes 0)
+#pragma unroll
+        for (int i = 0; i < kN; ++i) q[i] = finite ? (uint32_t)(int)fminf(fmaxf(rintf(w.at(i) * inverse), -63.f), 63.f) : 0;
+      }
       write_codes<kN>(p.Q + r * p.ldq + c, p.width - c, q);
       if (lane % kLanes == 0) p.exponents[r * p.ld_exponents + c / kMoeBlock] = (uint8_t)e;
     }
@@ -166,20 +218,27 @@ __global__ __launch_bounds__(256) void k_moe_unpack(Rows8 p, int32_t act) {
   constexpr int kN = Word<T>::kN;
   const bool gated = act == SPTIR_ACT_SWIGLU;
   const int lane = threadIdx.x & (p.lanes - 1), width = gated ? p.width / 2 : p.width;
-  const int64_t groups = (int64_t)gridDim.x * (256 / p.lanes);
-  for (int64_t r = (int64_t)blockIdx.x * (256 / p.lanes) + threadIdx.x / p.lanes; r < p.n_rows; r += groups) {
+  const int64_t groups = (int64_t)gridDim.x << (8 - p.shift);
+  for (int64_t r = ((int64_t)blockIdx.x << (8 - p.shift)) + (threadIdx.x >> p.shift); r < p.n_rows; r += groups) {
     const int8_t* q = p.Q + r * p.ldq;
     const uint8_t* e = p.exponents + r * p.ld_exponents;
     for (int c = lane * kN; c < width; c += p.lanes * kN) {
       float v[kN], u[kN];
-      read_kept<kN, true>(q, e, c, width - c, v);
+      Kept<kN, true> kept;
+      kept.read(q, e, c, width - c);
       if (gated) {
-        read_kept<kN, false>(q, e, width + c, width - c, u);
+        Kept<kN, false> pair;
+        pair.read(q, e, width + c, width - c);
+        pair.values(u);
+        kept.values(v);
 #pragma unroll
         for (int i = 0; i < kN; ++i) v[i] = act_gated<T>(v[i], u[i]);
-      } else if (act == SPTIR_ACT_RELU) act_word<T, SPTIR_ACT_RELU>(v);
-      else if (act == SPTIR_ACT_GELU) act_word<T, SPTIR_ACT_GELU>(v);
-      else if (act == SPTIR_ACT_SILU) act_word<T, SPTIR_ACT_SILU>(v);
+      } else {
+        kept.values(v);
+        if (act == SPTIR_ACT_RELU) act_word<T, SPTIR_ACT_RELU>(v);
+        else if (act == SPTIR_ACT_GELU) act_word<T, SPTIR_ACT_GELU>(v);
+        else if (act == SPTIR_ACT_SILU) act_word<T, SPTIR_ACT_SILU>(v);
+      }
       T o[kN];
 #pragma unroll
       for (int i = 0; i < kN; ++i) o[i] = from_float<T>(v[i]);
@@ -195,6 +254,8 @@ dim3 rows8_grid(int64_t words, Rows8* p) {
   p->lanes = 8;
   while (p->lanes < 64 && p->lanes < words) p->lanes *= 2;
   if (words > 256) p->lanes = 256;
+  p->shift = 0;
+  while (1 << p->shift < p->lanes) ++p->shift;
   const int64_t each = 256 / p->lanes;
   return dim3((unsigned)std::min<int64_t>((p->n_rows + each - 1) / each, 16384));
 }

@@ -140,14 +140,13 @@ __device__ inline void write_8(T* p, int32_t many, const float (&v)[8]) {
     }
   }
 }
-// ... of a row that is kept in 8 bits, from column j on (kOne: all in one block): as T they are what they stand for, exactly
+// ... of a row that is kept in 8 bits: as T they are what they stand for, exactly
 template <typename T, bool kOne>
-__device__ inline Eight<T> kept_8(const int8_t* codes, const uint8_t* exponents, int64_t j, int32_t many) {
+__device__ inline Eight<T> kept_8(const Kept<8, kOne>& kept) {
   constexpr int kN = Eight<T>::kN;
-  Eight<T> e = {};
-  if (many <= 0) return e;
+  Eight<T> e;
   float v[8];
-  read_kept<8, kOne>(codes, exponents, j, many, v);
+  kept.values(v);
 #pragma unroll
   for (int i = 0; i < 8; ++i) e.w[i / kN][i % kN] = from_float<T>(v[i]);
   return e;

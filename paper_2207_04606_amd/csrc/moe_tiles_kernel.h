@@ -63,10 +63,14 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // Eight elements along r for the lane's row, out of lines across: two transposing reads of four r each.  A group of 16 lanes
 // reads four lines of 16 elements, lane 4 x + w the w-th four of line x, and lane i gets element i of all four lines.
+// (__restrict__: what is known of such a read is then no less than of a plain one, before which the compiler inserts no wait for loads that
+// write LDS.  That they are there is what arrive_and_meet() sees to, for both kinds.)
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+__device__ inline s16x4 read_tr_4(lds_s16x4* __restrict__ a) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(a); }
 template <typename F>
 __device__ inline F read_tr(lds_char* a, int apart) {
-  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)a);
-  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(a + apart));
+  const s16x4 lo = read_tr_4((lds_s16x4*)a);
+  const s16x4 hi = read_tr_4((lds_s16x4*)(a + apart));
   const __attribute__((ext_vector_type(8))) short both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   return __builtin_bit_cast(F, both);
 }
@@ -501,7 +505,11 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
     } else {
       const bool other_too = kOp == kMoeForward ? p.residual != nullptr : kOp == kMoeDx && kEnd != kEndNone;
       Eight<O> bias[2] = {}, other[2][2] = {}, pair[2][2] = {};  // (what there is none of adds zeros)
-      constexpr int kAtOnce = kOp == kMoeDx && kEnd == kEndSwiglu ? 1 : 2;  // (what is read is twice as much there)
+      // (what is read is twice as much with swiglu; of 8 bits it is half as much, and as much as it takes for a wait the less)
+      constexpr int kAtOnce = kKept && kWords ? 4 : kOp == kMoeDx && kEnd == kEndSwiglu ? 1 : 2;
+      constexpr bool kPairOne = kWords && sizeof(O) == 2;  // (columns by eight: none of them lie in two blocks)
+      Kept<8, true> kept[kKept ? kAtOnce : 1][2] = {};
+      Kept<8, kPairOne> kept_pair[kKept ? kAtOnce : 1][2] = {};
       each<S::kFM / kAtOnce>([&](auto fs) {
         if (kOp == kMoeForward && p.bias) {
           const O* at = (const O*)p.bias + done.expert * p.bias_stride + my_j;
@@ -516,8 +524,11 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
               if constexpr (kKept) {
                 const int8_t* codes = (const int8_t*)p.pre + i * other_ld;
                 const uint8_t* exponents = p.exponents + i * p.ld_exponents;
-                other[f][x] = kept_8<O, true>(codes, exponents, my_j + x * 8, out_cols - my_j - x * 8);
-                if constexpr (kEnd == kEndSwiglu) pair[f][x] = kept_8<O, kWords && sizeof(O) == 2>(codes, exponents, (int64_t)my_j + x * 8 + p.n_j, out_cols - my_j - x * 8);
+                const int32_t j = my_j + x * 8;
+                if (j < out_cols) {
+                  kept[f][x].read(codes, exponents, j, out_cols - j);
+                  if constexpr (kEnd == kEndSwiglu) kept_pair[f][x].read(codes, exponents, (int64_t)j + p.n_j, out_cols - j);
+                }
               } else {
                 other[f][x] = read_8<O, kWords>(at + x * 8, out_cols - my_j - x * 8);
                 if constexpr (kOp == kMoeDx && kEnd == kEndSwiglu) pair[f][x] = read_8<O, kWords>(at + x * 8 + p.n_j, out_cols - my_j - x * 8);
@@ -552,7 +563,11 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
             each<2>([&](auto x) {
               const int32_t j = my_j + x * 8;
               if (j >= out_cols) return;
-              moe_emit_8<O, kOp, kEnd, kWords>(p, act, done.expert, i, j, out_cols - j, v + x * 8, bias[x], other[ff][x], pair[ff][x]);
+              if constexpr (kKept) {
+                other[0][x] = kept_8<O, true>(kept[ff][x]);
+                if constexpr (kEnd == kEndSwiglu) pair[0][x] = kept_8<O, kPairOne>(kept_pair[ff][x]);
+              }
+              moe_emit_8<O, kOp, kEnd, kWords>(p, act, done.expert, i, j, out_cols - j, v + x * 8, bias[x], other[kKept ? 0 : (int)ff][x], pair[kKept ? 0 : (int)ff][x]);
             });
           }
         });
