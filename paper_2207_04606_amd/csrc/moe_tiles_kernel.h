@@ -255,7 +255,16 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
       each<kLoadsB>([&](auto n) { entry[n] = p.entry_of[min(r0 + (int64_t)step * kBR + b_line(n), r1 - 1)]; });
     }
   };
-  auto x_row = [&](int step, int n) { return p.entry_of ? moe_token(p, entry[n]) : r0 + (int64_t)step * kBR + b_line(n); };
+  // (Their tokens are known before a step's first load is asked for: the wait for the entries would be one for that load too, 32,768 rows
+  // gathered for dW of 2048 x 1024 and 32 experts 305 -> 207 us.)
+  uint32_t x_row[kOp == kMoeDw ? kLoadsB : 1] = {};
+  auto find_rows = [&](int step) __attribute__((always_inline)) {
+    each<kLoadsB>([&](auto n) {
+      x_row[n] = (uint32_t)(p.entry_of ? moe_token(p, entry[n]) : r0 + (int64_t)step * kBR + b_line(n));
+      asm volatile("" : "+v"(x_row[n]));
+    });
+    __builtin_amdgcn_sched_barrier(0);
+  };
   // (without kWords) the length of the n-th chunk's line, and how far the chunk's end is past its end
   auto line_length = [&](int n) { return n < kLoadsA ? (kAAlongR ? p.n_r : p.n_i) : (kBAlongR ? p.n_r : p.n_j); };
   auto past_end = [&](int step, int n) {
@@ -274,13 +283,13 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
     const int r = kAlong ? chunk * kN : line;
     if constexpr (kWords) {
       const char* at = (kA ? a_base : b_base) + (uint64_t)place[n] * 16;
-      if constexpr (!kA && kOp == kMoeDw) at += x_row(step, m) * p.ldb * (int64_t)sizeof(T);
+      if constexpr (!kA && kOp == kMoeDw) at += (int64_t)x_row[m] * p.ldb * (int64_t)sizeof(T);
       if (!whole && r >= left) at = (const char*)g_zero;
       to_lds(at, lds + into * S::kStage + (n * kThreads + wave * 64) * 16);
     } else {
       // (the line's last 16 bytes where it ends before the chunk does: put() moves them to their place)
       const T* at = from[n];
-      if constexpr (!kA && kOp == kMoeDw) at += x_row(step, m) * p.ldb;
+      if constexpr (!kA && kOp == kMoeDw) at += (int64_t)x_row[m] * p.ldb;
       const bool there = kAlong || whole || r < left;
       const int over = past_end(step, n);
       if (line_length(n) >= kN) {
@@ -294,6 +303,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   };
   auto load = [&](int step, int into) __attribute__((always_inline)) {
     const bool whole = kWords && (int64_t)(step + 1) * kBR <= r1 - r0;
+    if constexpr (kOp == kMoeDw) find_rows(step);
     if (whole) each<kLoads>([&](auto n) { load_one(step, into, n, std::true_type{}); });
     else each<kLoads>([&](auto n) { load_one(step, into, n, std::false_type{}); });
     if constexpr (kWords) {
