@@ -381,10 +381,19 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
     }
   };
   auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
-  auto multiply = [&](auto set, auto phase) __attribute__((always_inline)) {
+  auto multiply_one = [&](auto set, auto phase, auto f, auto g) __attribute__((always_inline)) {
     constexpr int ph = decltype(phase)::value, kSet = decltype(set)::value;
+    acc[ph * 2 + f][g] = M::run(b[kSet][g], a[ph & 1][f], acc[ph * 2 + f][g]);
+  };
+  auto multiply_first = [&](auto set, auto phase) __attribute__((always_inline)) {
+    multiply_one(set, phase, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
+  };
+  auto multiply_rest = [&](auto set, auto phase) __attribute__((always_inline)) {
+    constexpr int ph = decltype(phase)::value;
     each<2>([&](auto f) {
-      each<4>([&](auto g) { acc[ph * 2 + f][g] = M::run(b[kSet][g], a[ph & 1][f], acc[ph * 2 + f][g]); });
+      each<4>([&](auto g) {
+        if constexpr (decltype(f)::value + decltype(g)::value > 0) multiply_one(set, phase, f, g);
+      });
     });
     if constexpr (kSumZ) {  // dZ times ones: the wavefronts that share rows take a phase's each
       if (sum_z && wn == ph % S::kWavesN) {
@@ -414,17 +423,21 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
       constexpr std::integral_constant<int, kk> set{};
       constexpr std::integral_constant<int, kk ^ 1> other{};
       each<kPhases - 1>([&](auto phase) {
+        multiply_first(set, phase);
+        fence();
         read_rows(stage, kk, std::integral_constant<int, decltype(phase)::value + 1>{});
         fence();
-        multiply(set, phase);
+        multiply_rest(set, phase);
         fence();
       });
       constexpr std::integral_constant<int, kPhases - 1> last{};
       if constexpr (kk + 1 < kHalves) {
+        multiply_first(set, last);
+        fence();
         read_cols(stage, kk + 1, other);
         read_rows(stage, kk + 1, Set0{});
         fence();
-        multiply(set, last);
+        multiply_rest(set, last);
         fence();
       } else {
         arrive_and_meet<kWords ? 0 : kNoWait>();
@@ -439,7 +452,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
           if (s + 2 < steps) put(s + 2, stage);
           if (s + 3 < steps) load(s + 3, 0);
         }
-        multiply(set, last);
+        multiply_first(set, last);
+        multiply_rest(set, last);
         fence();
       }
     });
