@@ -15,6 +15,8 @@ __device__ inline float turned(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + kTurn, 0xf, 0xf, false));
 }
 template <int kTurn>
+__device__ inline int32_t turned(int32_t v) { return __builtin_amdgcn_update_dpp(0, v, 0x120 + kTurn, 0xf, 0xf, false); }
+template <int kTurn>
 __device__ inline double turned(double v) {
   const uint64_t b = __builtin_bit_cast(uint64_t, v);
   const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)b, 0x120 + kTurn, 0xf, 0xf, false);
@@ -36,7 +38,11 @@ __device__ inline V over_lanes(V v, F&& f) {
 }
 template <int L, typename V>
 __device__ inline V lanes_max(V v) {
-  return over_lanes<L>(v, [](V a, V b) { return sizeof(V) == 8 ? (V)fmax((double)a, (double)b) : (V)fmaxf((float)a, (float)b); });
+  return over_lanes<L>(v, [](V a, V b) {
+    if constexpr (std::is_same_v<V, int32_t>) return a > b ? a : b;
+    else if constexpr (sizeof(V) == 8) return fmax(a, b);
+    else return fmaxf(a, b);
+  });
 }
 template <int L, typename V>
 __device__ inline V lanes_sum(V v) {

@@ -1,9 +1,8 @@
 // The router with scores of its own kind: softmax or sigmoids, a bias that moves the choice but not the weights, groups of experts
 // of which a token may use some, weights renormalised and scaled; and its gradient.
 //
-// Which expert comes first is decided in float64 (the header says so): scores and bias are added there, since of 256 sigmoids of a token two
-// often lie closer than float32 tells once a bias is added, and a choice is a whole number.  What is compared is float32 all
-// the same: rounding keeps the order, so that only keys that are equal in float32 are looked at in float64.
+// Which expert comes first is decided in float64 (the header says so), since of 256 sigmoids of a token two often lie closer than float32 tells once a
+// bias is added, and a choice is a whole number.  Most tokens' choices are further apart, and are found in float32.
 #include "moe_lanes.h"
 
 namespace sptir {
@@ -24,19 +23,62 @@ struct Scoring {
   const float* bias;
 };
 
-// The best of a lane's keys and the lowest of its places; *alone: no other of them is equal.
-template <typename V, int C>
-__device__ inline V best_of(const V (&key)[C], int* at, bool* alone) {
-  V best = key[0];
-#pragma unroll
-  for (int c = 1; c < C; ++c) best = key[c] > best ? key[c] : best;
-  int many = 0;
-  *at = 0;
-#pragma unroll
-  for (int c = C - 1; c >= 0; --c)
-    if (key[c] == best) { *at = c; ++many; }
-  *alone = many == 1;
-  return best;
+// ---- the choice in float32, where it is that of float64
+// A key is c with the last four bits taken for a mark, by which the largest of a lane's keys is the one of the lowest number.  Errors: a sigmoid
+// 2^-21 s, a softmax 2^-21 s and 2^-24 times its exponent (up to 70, for keys of 2^-100 and more) more, the sum 2^-24 |c|, the mark 2^-19 |c|.  So two
+// keys that are further apart than 2^-16 of the larger one, or with a bias than 2^-17 (1 + the larger one), say how c lie.  Tokens with two choices
+// closer than that (of 256 experts one in a few hundred) are chosen from in float64, with the other tokens of the wavefront.
+// Logits of 16 bits without a bias are keys themselves, and ties are ties: a mark takes nothing from them.  Float64 tells their scores
+// apart while exponents are within +- 600, sigmoids' logits below 30 and differences not below 2^-40.
+constexpr float kFar = 0x1p100f;  // past all keys
+constexpr float kMost = 0x1p90f;  // keys are cut off here, and a choice past 2^80 is left to float64
+constexpr float kFloor = 0x1p-100f;  // of scores without a bias: those that are smaller are alike here
+// A float32 as a whole number with the same order, its last four bits for the mark, and back without it
+template <int C>
+__device__ inline int32_t marked_key(float v, int c) {
+  static_assert(C <= 16, "four bits");
+  const int32_t bits = __builtin_bit_cast(int32_t, v), in_order = bits ^ ((bits >> 31) & 0x7fffffff);
+  return (in_order & ~15) | (15 - c);
+}
+__device__ inline float of_key(int32_t cut) { return __builtin_bit_cast(float, cut ^ ((cut >> 31) & 0x7fffffff)); }
+
+// The bits of a token's L lanes
+template <int L>
+__device__ inline unsigned long long lanes_of(unsigned long long ballot, int base) {
+  const unsigned long long mine = ballot >> base;
+  return L == 64 ? mine : mine & 0xffff;
+}
+
+// The groups that stay, as bits, from their scores in LDS; *close: two scores are no further apart than `apart` and `rel` of one, so that the choice may be
+// another one.
+template <int L, typename V>
+__device__ inline unsigned long long staying_groups(const V* scores, V none, int n_groups, int top_groups, int lane, int base, V apart, V rel, bool* close) {
+  unsigned long long stay = 0;
+  bool near = false;
+  for (int g0 = 0; g0 < n_groups; g0 += L) {
+    const int g = g0 + lane;
+    int before = kMoeMaxGroups;
+    if (g < n_groups) {
+      const V v = scores[g];
+      before = v == none ? kMoeMaxGroups : 0;
+#pragma unroll 8
+      for (int o = 0; o < n_groups; ++o) {
+        const V other = scores[o];
+        before += other > v || (other == v && o < g);
+        const V margin = apart + rel * (fabs(v) > fabs(other) ? fabs(v) : fabs(other));
+        near = near || (o != g && v != none && other - v <= margin && v - other <= margin);
+      }
+    }
+    stay |= lanes_of<L>(__ballot(before < top_groups), base) << g0;
+  }
+  *close = near;
+  return stay;
+}
+
+template <typename V>
+__device__ inline void take_two(V v, V& best, V& second) {
+  second = v > best ? best : v > second ? v : second;
+  best = v > best ? v : best;
 }
 
 // L lanes per token, lane l has the experts l * C .. l * C + C - 1 (as k_moe_route).
@@ -49,105 +91,186 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
   const int t = blockIdx.x * (256 / L) + threadIdx.x / L;
   if (t >= n_tokens) return;  // (whole groups of L lanes)
   const T* row = logits + (int64_t)t * ld;
-  float l[C];
-  double key[C], total = 1.0;
-  float most = -INFINITY;
+  const bool grouped = how.top_groups < how.n_groups;
+  const int each = n_experts / how.n_groups;
+  double* const mine = keys_of + threadIdx.x / L * (n_experts + how.n_groups);
+  const float inverse_each = 1.f / (float)each;  // ((e + 1/2) / each is at least 1/2048 from a whole number)
+  float l[C], b[C];
   read_logits<T, C>(row, first, n_experts, l);
-  if (how.sigmoid) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) key[c] = 1.0 / (1.0 + exp(-(double)l[c]));
-  } else {
-#pragma unroll
-    for (int c = 0; c < C; ++c) most = fmaxf(most, l[c]);  // (not the NaN)
-    most = lanes_max<L>(most);
-    double sum = 0.0;
-    bool nan = false;
+  for (int c = 0; c < C; ++c) b[c] = 0.f;
+  if (how.bias) read_logits<float, C>(how.bias, first, n_experts, b);
+  float most = -INFINITY;
+  bool nan = false;
+  if (!how.sigmoid) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      key[c] = l[c] == most ? 1.0 : l[c] > -INFINITY ? exp((double)l[c] - (double)most) : 0.0;
-      sum += key[c];
+      most = fmaxf(most, l[c]);  // (not the NaN)
       nan = nan || l[c] != l[c];
     }
-    sum = lanes_sum<L>(sum);
-    const double inverse = 1.0 / sum;
-#pragma unroll
-    for (int c = 0; c < C; ++c) key[c] *= inverse;
-    const unsigned long long any = __ballot(nan) >> base;
-    total = (L == 64 ? any : any & 0xffff) ? (double)NAN : sum;  // (of the weights, which a NaN reaches)
-  }
-  if (how.bias) {
-    float b[C];
-    read_logits<float, C>(how.bias, first, n_experts, b);
-#pragma unroll
-    for (int c = 0; c < C; ++c) key[c] += (double)b[c];
-  }
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-    if (!(l[c] > -INFINITY) || !(key[c] > -INFINITY)) key[c] = -INFINITY;
-
-  if (how.top_groups < how.n_groups) {
-    const int each = n_experts / how.n_groups;
-    double* mine = keys_of + threadIdx.x / L * (n_experts + how.n_groups);
-    double* scores = mine + n_experts;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (first + c < n_experts) mine[first + c] = key[c];
-    lds_meet();
-    for (int g = lane; g < how.n_groups; g += L) {
-      double best = -INFINITY, second = -INFINITY;
-#pragma unroll 8
-      for (int i = 0; i < each; ++i) {
-        const double v = mine[g * each + i];
-        second = fmax(second, fmin(best, v));
-        best = fmax(best, v);
-      }
-      scores[g] = how.group_top == 1 || second == -INFINITY ? best : best + second;
-    }
-    lds_meet();
-    unsigned long long stay = 0;  // the groups that do
-    for (int g0 = 0; g0 < how.n_groups; g0 += L) {
-      const int g = g0 + lane;
-      int before = kMoeMaxGroups;
-      if (g < how.n_groups) {
-        const double v = scores[g];
-        before = v == -INFINITY ? kMoeMaxGroups : 0;
-        for (int o = 0; o < how.n_groups; ++o) before += scores[o] > v || (scores[o] == v && o < g);
-      }
-      const unsigned long long here = __ballot(before < how.top_groups) >> base;
-      stay |= (L == 64 ? here : here & 0xffff) << g0;
-    }
-    const float inverse = 1.f / (float)each;  // ((e + 1/2) / each is at least 1/2048 from a whole number)
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (!(stay >> (int)(((float)(first + c) + 0.5f) * inverse) & 1)) key[c] = -INFINITY;
+    most = lanes_max<L>(most);
   }
 
-  float near[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) near[c] = (float)key[c];
+  // ---- in float32
   int id = -1;  // the choice of this lane's number
-  for (int j = 0; j < top_k; ++j) {
-    int at;
-    bool alone;
-    const float best = best_of(near, &at, &alone);
-    const float top = lanes_max<L>(best);
-    unsigned long long tied = __ballot(best == top) >> base;
-    if (L != 64) tied &= 0xffff;
-    int owner = __ffsll(tied) - 1;
-    bool some = top > -INFINITY;
-    if (__ballot(some && best == top && (!alone || (tied & (tied - 1))))) {  // (for all tokens of the wavefront: it gives the same)
-      const double exact = best_of(key, &at, &alone), highest = lanes_max<L>(exact);
-      tied = __ballot(exact == highest) >> base;
-      if (L != 64) tied &= 0xffff;
-      owner = __ffsll(tied) - 1;
-      some = highest > -INFINITY;
-    }
-    // (the owner's expert to all lanes, as a float: below 2^24)
-    const float e = lanes_max<L>(lane == owner ? (float)(first + at) : -1.f);
-    if (lane == j && some) id = (int)e;
+  bool unsure = false;
+  double total = 1.0;
+  {
+    float key[C], size = 0.f;
+    if (how.sigmoid) {
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (lane == owner && c == at) { near[c] = -INFINITY; key[c] = -INFINITY; }
+      for (int c = 0; c < C; ++c) key[c] = __builtin_amdgcn_rcpf(1.f + expf(-l[c]));
+    } else {
+      double sum = 0.0;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        key[c] = l[c] > -INFINITY ? expf(l[c] - most) : 0.f;
+        sum += (double)key[c];
+      }
+      sum = lanes_sum<L>(sum);
+      const float inverse = __builtin_amdgcn_rcpf((float)sum);
+#pragma unroll
+      for (int c = 0; c < C; ++c) key[c] *= inverse;
+      // (for weights that are not normalised: the choice knows no NaN, they do)
+      total = lanes_of<L>(__ballot(nan), base) ? (double)NAN : sum;
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const bool there = l[c] > -INFINITY && b[c] > -INFINITY;  // (c would be NaN, or -inf, with such a bias)
+      const float v = key[c] + b[c];
+      unsure = unsure || (there && v != v);
+      size = fmaxf(size, b[c]);
+      key[c] = !there ? -kFar : fminf(fmaxf(v, how.bias ? -kMost : kFloor), kMost);
+    }
+    if (grouped) {
+      float* scores = (float*)mine;
+      float best = -kFar, second = -kFar;
+      const int lanes = each / C;
+      if (lanes * C == each && (lanes & (lanes - 1)) == 0) {  // a group is 1, 2, 4 .. lanes
+#pragma unroll
+        for (int c = 0; c < C; ++c) take_two(key[c], best, second);
+        for (int d = 1; d < lanes; d <<= 1) {
+          const float other = __shfl_xor(best, d), next = __shfl_xor(second, d);
+          take_two(other, best, second);
+          take_two(next, best, second);
+        }
+        if ((lane & (lanes - 1)) == 0 && first < n_experts) scores[lane / lanes] = how.group_top == 1 || second == -kFar ? best : best + second;
+        lds_meet();
+      } else {
+        float* keys = scores + how.n_groups;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          if (first + c < n_experts) keys[first + c] = key[c];
+        lds_meet();
+        for (int g = lane; g < how.n_groups; g += L) {
+          best = second = -kFar;
+#pragma unroll 8
+          for (int i = 0; i < each; ++i) take_two(keys[g * each + i], best, second);
+          scores[g] = how.group_top == 1 || second == -kFar ? best : best + second;
+        }
+        lds_meet();
+      }
+      bool close;
+      // (a score is a sum of two, which may cancel: the larger is at most 1 + the largest bias, the other's size no more than that and the score's)
+      const float apart = how.bias ? 0x1p-15f * (1.f + lanes_max<L>(size)) : 0.f;
+      const unsigned long long stay = staying_groups<L>(scores, -kFar, how.n_groups, how.top_groups, lane, base, apart, 0x1p-16f, &close);
+      unsure = unsure || close;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        if (!(stay >> (int)(((float)(first + c) + 0.5f) * inverse_each) & 1)) key[c] = -kFar;
+    }
+    const bool logit_keys = sizeof(T) == 2 && !how.bias;
+    if (logit_keys) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) key[c] = key[c] == -kFar ? -kFar : fminf(fmaxf(l[c], -kMost), kMost);
+    }
+    int32_t order[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) order[c] = marked_key<C>(key[c], c);
+    // one choice more than there are, for the distance of the last
+    float last = 0.f;
+    for (int j = 0; j <= top_k; ++j) {
+      int32_t best = order[0];
+#pragma unroll
+      for (int c = 1; c < C; ++c) best = max(best, order[c]);
+      const int32_t cut = best & ~15, most_cut = lanes_max<L>(cut);
+      const int owner = __ffsll(lanes_of<L>(__ballot(cut == most_cut), base)) - 1;
+      const int at = 15 - (lanes_max<L>(lane == owner ? best : INT32_MIN) & 15);
+      const float top = of_key(most_cut);
+      const bool some = top > -0.5f * kFar;
+      if (logit_keys) {
+        const float exponent = how.sigmoid ? top : top - most;
+        unsure = unsure || (some && (!(fabsf(exponent) < 600.f) || (how.sigmoid && top > 30.f) || (j > 0 && top != last && last - top < 0x1p-40f)));
+      } else {
+        const float larger = fmaxf(fabsf(last), fabsf(top));
+        unsure = unsure || (some && (larger > 0x1p80f || (j > 0 && !(last - top > (how.bias ? 0x1p-17f * (1.f + larger) : 0x1p-16f * larger)))));
+      }
+      last = top;
+      if (lane == j && some) id = owner * C + at;
+      const int32_t taken = lane == owner ? best : INT32_MIN;
+#pragma unroll
+      for (int c = 0; c < C; ++c) order[c] = order[c] == taken ? INT32_MIN : order[c];
+    }
+    if (lane >= top_k) id = -1;
+  }
+
+  // ---- in float64, all tokens of the wavefront
+  if (__ballot(unsure)) {
+    double key[C];
+    if (how.sigmoid) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) key[c] = 1.0 / (1.0 + exp(-(double)l[c]));
+    } else {
+      double sum = 0.0;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        key[c] = l[c] == most ? 1.0 : l[c] > -INFINITY ? exp((double)l[c] - (double)most) : 0.0;
+        sum += key[c];
+      }
+      const double inverse = 1.0 / lanes_sum<L>(sum);
+#pragma unroll
+      for (int c = 0; c < C; ++c) key[c] *= inverse;
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      key[c] += (double)b[c];
+      if (!(l[c] > -INFINITY) || !(key[c] > -INFINITY)) key[c] = -INFINITY;
+    }
+    if (grouped) {
+      double* scores = mine + n_experts;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        if (first + c < n_experts) mine[first + c] = key[c];
+      lds_meet();
+      for (int g = lane; g < how.n_groups; g += L) {
+        double best = -INFINITY, second = -INFINITY;
+#pragma unroll 8
+        for (int i = 0; i < each; ++i) take_two(mine[g * each + i], best, second);
+        scores[g] = how.group_top == 1 || second == -INFINITY ? best : best + second;
+      }
+      lds_meet();
+      bool close;
+      const unsigned long long stay = staying_groups<L>(scores, (double)-INFINITY, how.n_groups, how.top_groups, lane, base, -1.0, 0.0, &close);
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        if (!(stay >> (int)(((float)(first + c) + 0.5f) * inverse_each) & 1)) key[c] = -INFINITY;
+    }
+    id = -1;
+    for (int j = 0; j < top_k; ++j) {
+      double best = key[0];
+      int at = 0;
+#pragma unroll
+      for (int c = 1; c < C; ++c)
+        if (key[c] > best) { best = key[c]; at = c; }
+      const double top = lanes_max<L>(best);
+      const int owner = __ffsll(lanes_of<L>(__ballot(best == top), base)) - 1;
+      // (the owner's expert to all lanes, as a float: below 2^24)
+      const float e = lanes_max<L>(lane == owner ? (float)(first + at) : -1.f);
+      if (lane == j && top > -INFINITY) id = (int)e;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        if (lane == owner && c == at) key[c] = -INFINITY;
+    }
   }
 
   // The weights: s = exp(min(l, 0)) / (1 + exp(-|l|)) for sigmoids; what they are divided by keeps the largest of the exponents at 0.
@@ -175,6 +298,7 @@ __global__ __launch_bounds__(256) void k_moe_route_groups_backward(const T* __re
                                                                    int32_t n_experts, int32_t top_k, Scoring how,
                                                                    const int32_t* __restrict__ experts, const float* __restrict__ weights,
                                                                    const float* __restrict__ d_weights, T* __restrict__ d_logits, int64_t ld_d) {
+  extern __shared__ __attribute__((aligned(16))) float gradients[];
   const int lane = threadIdx.x & (L - 1);
   const int t = blockIdx.x * (256 / L) + threadIdx.x / L;
   if (t >= n_tokens) return;
@@ -191,12 +315,12 @@ __global__ __launch_bounds__(256) void k_moe_route_groups_backward(const T* __re
   const float m = lanes_sum<L>(w * dw), mean = how.scale != 0.f ? m / how.scale : 0.f;
   float of_choice = w * (how.normalise || !how.sigmoid ? dw - mean : dw);
   if (how.sigmoid && id >= 0) of_choice *= 1.f / (1.f + expf(to_float(row[id])));
-  float d[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) d[c] = 0.f;
+  // the token's gradients in LDS, for which its choices have no other place to meet; from there in 16-byte words
+  float* const mine = gradients + threadIdx.x / L * ((n_experts + 3) & ~3);
   if (!how.normalise && !how.sigmoid) {
+    const int first = lane * C;
     float l[C], top = -INFINITY, all = 0.f;
-    read_logits<T, C>(row, lane * C, n_experts, l);
+    read_logits<T, C>(row, first, n_experts, l);
 #pragma unroll
     for (int c = 0; c < C; ++c) top = fmaxf(top, l[c]);
     top = lanes_max<L>(top);
@@ -206,19 +330,26 @@ __global__ __launch_bounds__(256) void k_moe_route_groups_backward(const T* __re
       all += l[c];
     }
     all = lanes_sum<L>(all);
-    if (all != 0.f) {  // (a token without any choice: 0)
-#pragma unroll
-      for (int c = 0; c < C; ++c) d[c] = -(l[c] / all) * m;
-    }
-  }
-  for (int j = 0; j < top_k; ++j) {
-    const int e = __shfl(id, j, L);
-    const float g = __shfl(of_choice, j, L);
 #pragma unroll
     for (int c = 0; c < C; ++c)
-      if (e == lane * C + c) d[c] = g;
+      if (first + c < n_experts) mine[first + c] = all != 0.f ? -(l[c] / all) * m : 0.f;  // (a token without any choice: 0)
+  } else {
+    const float zero[4] = {};
+    for (int e = lane * 4; e < n_experts; e += L * 4) __builtin_memcpy(__builtin_assume_aligned(mine + e, 16), zero, 16);
   }
-  write_logits<T, C>(d_logits + (int64_t)t * ld_d, lane * C, n_experts, d);
+  lds_meet();
+  if (id >= 0) mine[id] = of_choice;
+  lds_meet();
+  constexpr int kN = 16 / sizeof(T);
+  T* out = d_logits + (int64_t)t * ld_d;
+  for (int e = lane * kN; e < n_experts; e += L * kN) {
+    T v[kN];
+#pragma unroll
+    for (int i = 0; i < kN; ++i) v[i] = from_float<T>(mine[min(e + i, n_experts - 1)]);
+    u32x4 word;
+    __builtin_memcpy(&word, v, 16);
+    write_word(out + e, word, n_experts - e);
+  }
 }
 
 sptir_status_t check_scoring(const sptir_moe_scoring_t* s, int32_t n_tokens, int32_t top_k, int32_t n_experts, Scoring* how) {
@@ -280,7 +411,9 @@ extern "C" sptir_status_t sptir_moe_route_groups_backward(const void* logits, in
     with_lanes(n_experts, top_k, [&](auto l, auto c) {
       constexpr int kLanes = decltype(l)::value;
       in_launches(n_tokens, kLanes, [&](int64_t t, int32_t n, dim3 grid) {
-        hipLaunchKernelGGL((k_moe_route_groups_backward<T, kLanes, decltype(c)::value>), grid, dim3(256), 0, (hipStream_t)stream,
+        // (16 tokens of 256 experts or 4 of 1024: 16 KB)
+        const size_t lds = sizeof(float) * (256 / kLanes) * ((n_experts + 3) & ~3);
+        hipLaunchKernelGGL((k_moe_route_groups_backward<T, kLanes, decltype(c)::value>), grid, dim3(256), lds, (hipStream_t)stream,
                            (const T*)logits + t * ld_logits, ld_logits, n, n_experts, top_k, how, experts + t * top_k, weights + t * top_k,
                            d_weights + t * top_k, (T*)d_logits + t * ld_d_logits, ld_d_logits);
       });

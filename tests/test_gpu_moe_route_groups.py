@@ -48,8 +48,10 @@ def test_route_groups(gpu_lib, dtype, scores, normalise, scale, with_bias, T, E,
     want, w_want = ref8.route(l, k, bias=bias, **how)
     dev, experts, weights = run(gpu_lib, l, k, extra, bias=None if bias is None else bias.cuda(), **how)
     assert torch.equal(experts.cpu(), want)
-    # computed in float64 and rounded once
-    ref.check(weights, w_want, w_want.abs() * 2.0 ** -24 * 1.01 + 2.0 ** -149, "weights")
+    # computed in float64 and rounded once; the sum under a softmax that is not normalised is one of float32 exponentials: each within 2^-23 of
+    # its own and, for the rounding of its exponent d, d 2^-24, whose mean under the softmax is its entropy less the log of the sum: below log E
+    near = 1.01 if scores == "sigmoid" or normalise else 1.01 + 2.0 + math.log(E)
+    ref.check(weights, w_want, w_want.abs() * 2.0 ** -24 * near + 2.0 ** -149, "weights")
     dw = randn(gen, T, k)
     dw[want < 0] = math.nan                                # of a choice that is none
     want_d = ref8.route_gradient(l, want, dw, scores, normalise, scale)
