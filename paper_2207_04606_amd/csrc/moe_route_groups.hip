@@ -27,7 +27,8 @@ struct Scoring {
 // A key is c with the last four bits taken for a mark, by which the largest of a lane's keys is the one of the lowest number.  Errors: a sigmoid
 // 2^-21 s, a softmax 2^-21 s and 2^-24 times its exponent (up to 70, for keys of 2^-100 and more) more, the sum 2^-24 |c|, the mark 2^-19 |c|.  So two
 // keys that are further apart than 2^-16 of the larger one, or with a bias than 2^-17 (1 + the larger one), say how c lie.  Tokens with two choices
-// closer than that (of 256 experts one in a few hundred) are chosen from in float64, with the other tokens of the wavefront.
+// closer than that (of 256 experts one in a hundred) are put in order by float64; those whose groups are, or whose keys float32 has no room for, are chosen from in float64
+// altogether, with the other tokens of the wavefront.
 // Logits of 16 bits without a bias are keys themselves, and ties are ties: a mark takes nothing from them.  Float64 tells their scores
 // apart while exponents are within +- 600, sigmoids' logits below 30 and differences not below 2^-40.
 constexpr float kFar = 0x1p100f;  // past all keys
@@ -49,29 +50,35 @@ __device__ inline unsigned long long lanes_of(unsigned long long ballot, int bas
   return L == 64 ? mine : mine & 0xffff;
 }
 
-// The groups that stay, as bits, from their scores in LDS; *close: two scores are no further apart than `apart` and `rel` of one, so that the choice may be
-// another one.
+// The groups that stay, as bits, from their scores in LDS; *gap: how much less the best of the others has than the last of them, *size: the larger magnitude of both.
 template <int L, typename V>
-__device__ inline unsigned long long staying_groups(const V* scores, V none, int n_groups, int top_groups, int lane, int base, V apart, V rel, bool* close) {
+__device__ inline unsigned long long staying_groups(const V* scores, V none, int n_groups, int top_groups, int lane, int base, V* gap, V* size) {
   unsigned long long stay = 0;
-  bool near = false;
+  V lowest = (V)INFINITY, highest = none;
   for (int g0 = 0; g0 < n_groups; g0 += L) {
     const int g = g0 + lane;
     int before = kMoeMaxGroups;
+    V v = none;
     if (g < n_groups) {
-      const V v = scores[g];
+      v = scores[g];
       before = v == none ? kMoeMaxGroups : 0;
 #pragma unroll 8
       for (int o = 0; o < n_groups; ++o) {
         const V other = scores[o];
         before += other > v || (other == v && o < g);
-        const V margin = apart + rel * (fabs(v) > fabs(other) ? fabs(v) : fabs(other));
-        near = near || (o != g && v != none && other - v <= margin && v - other <= margin);
       }
     }
-    stay |= lanes_of<L>(__ballot(before < top_groups), base) << g0;
+    const bool stays = before < top_groups;
+    if (stays) lowest = v < lowest ? v : lowest;
+    else highest = v > highest ? v : highest;
+    stay |= lanes_of<L>(__ballot(stays), base) << g0;
   }
-  *close = near;
+  if (gap) {
+    lowest = -lanes_max<L>(-lowest);
+    highest = lanes_max<L>(highest);
+    *gap = highest == none ? (V)INFINITY : lowest - highest;
+    *size = fabs(lowest) > fabs(highest) ? fabs(lowest) : fabs(highest);
+  }
   return stay;
 }
 
@@ -86,7 +93,7 @@ template <typename T, int L, int C>
 __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ logits, int64_t ld, int32_t n_tokens, int32_t n_experts,
                                                           int32_t top_k, Scoring how, int32_t* __restrict__ experts,
                                                           float* __restrict__ weights) {
-  extern __shared__ double keys_of[];  // a token's keys and its groups' scores, where groups are chosen from
+  extern __shared__ double keys_of[];  // a token's keys and its groups' scores
   const int lane = threadIdx.x & (L - 1), first = lane * C, base = (threadIdx.x & 63) - lane;
   const int t = blockIdx.x * (256 / L) + threadIdx.x / L;
   if (t >= n_tokens) return;  // (whole groups of L lanes)
@@ -170,11 +177,12 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
         }
         lds_meet();
       }
-      bool close;
-      // (a score is a sum of two, which may cancel: the larger is at most 1 + the largest bias, the other's size no more than that and the score's)
-      const float apart = how.bias ? 0x1p-15f * (1.f + lanes_max<L>(size)) : 0.f;
-      const unsigned long long stay = staying_groups<L>(scores, -kFar, how.n_groups, how.top_groups, lane, base, apart, 0x1p-16f, &close);
-      unsure = unsure || close;
+      float gap, size_of_both;
+      const unsigned long long stay = staying_groups<L>(scores, -kFar, how.n_groups, how.top_groups, lane, base, &gap, &size_of_both);
+      // (A score is a sum of two, which may cancel: the larger is at most 1 + the largest bias B, the other's size no more than that and the score's.  So of
+      // two scores, each of two sigmoids within 2^-21.9 and three roundings of sums, the distance is within 2^-19.9 + 2^-22 (1 + B) + 2^-22 of the larger; softmaxes 2^-21.)
+      const float apart = how.bias ? (how.sigmoid ? 0x1p-19f : 0x1p-18f) * (1.f + fmaxf(lanes_max<L>(size), 0.f)) + 0x1p-21f * size_of_both : 0x1p-16f * size_of_both;
+      unsure = unsure || !(gap > apart);
 #pragma unroll
       for (int c = 0; c < C; ++c)
         if (!(stay >> (int)(((float)(first + c) + 0.5f) * inverse_each) & 1)) key[c] = -kFar;
@@ -187,9 +195,11 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
     int32_t order[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) order[c] = marked_key<C>(key[c], c);
-    // one choice more than there are, for the distance of the last
+    // One choice more than there are, for the distance of the last; as long as it is too close, one more.  The choices are the lanes'.
     float last = 0.f;
-    for (int j = 0; j <= top_k; ++j) {
+    bool tight = false, more = true;
+    int many = 0;  // choices that are further apart from the rest
+    for (int j = 0;; ++j) {
       int32_t best = order[0];
 #pragma unroll
       for (int c = 1; c < C; ++c) best = max(best, order[c]);
@@ -198,50 +208,77 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
       const int at = 15 - (lanes_max<L>(lane == owner ? best : INT32_MIN) & 15);
       const float top = of_key(most_cut);
       const bool some = top > -0.5f * kFar;
-      if (logit_keys) {
+      bool apart = j > 0;
+      if (some && logit_keys) {
         const float exponent = how.sigmoid ? top : top - most;
-        unsure = unsure || (some && (!(fabsf(exponent) < 600.f) || (how.sigmoid && top > 30.f) || (j > 0 && top != last && last - top < 0x1p-40f)));
-      } else {
+        unsure = unsure || (more && (!(fabsf(exponent) < 600.f) || (how.sigmoid && top > 30.f) || (j > 0 && top != last && last - top < 0x1p-40f)));
+      } else if (some) {
         const float larger = fmaxf(fabsf(last), fabsf(top));
-        unsure = unsure || (some && (larger > 0x1p80f || (j > 0 && !(last - top > (how.bias ? 0x1p-17f * (1.f + larger) : 0x1p-16f * larger)))));
+        unsure = unsure || (more && larger > 0x1p80f);
+        apart = j > 0 && last - top > (how.bias ? 0x1p-17f * (1.f + larger) : 0x1p-16f * larger);
+        tight = tight || (more && j > 0 && !apart);
+      }
+      if (more && j >= top_k && (apart || !some)) {
+        many = j;
+        more = false;
+      }
+      if (!__ballot(more)) break;
+      if (j == L) {  // (no lane for one more)
+        unsure = unsure || more;
+        break;
       }
       last = top;
-      if (lane == j && some) id = owner * C + at;
+      if (lane == j && some && more) id = owner * C + at;
       const int32_t taken = lane == owner ? best : INT32_MIN;
 #pragma unroll
       for (int c = 0; c < C; ++c) order[c] = order[c] == taken ? INT32_MIN : order[c];
     }
+    // Those that are close are put in order by what they are in float64 (without a bias softmaxes by their exponentials).
+    unsure = unsure || (tight && !how.sigmoid && how.bias);
+    if (__ballot(tight)) {
+      double c64 = -INFINITY;
+      if (id >= 0) {
+        const double v = to_float(row[id]);
+        c64 = how.sigmoid ? 1.0 / (1.0 + exp(-v)) + (how.bias ? (double)how.bias[id] : 0.0) : exp(v - (double)most);
+      }
+      int rank = lane < many ? 0 : lane;
+      for (int o = 0; o < L; ++o) {
+        if (!__ballot(o < many)) break;
+        const double other = __shfl(c64, o, L);
+        const int other_id = __shfl(id, o, L);
+        // (places without a choice stay behind each other)
+        if (lane < many && o < many) rank += other > c64 || (other == c64 && (id < 0 || other_id < 0 ? o < lane : other_id < id));
+      }
+      // (every lane sends to another one)
+      id = __builtin_amdgcn_ds_permute((base + rank) * 4, id);
+    }
     if (lane >= top_k) id = -1;
   }
 
-  // ---- in float64, all tokens of the wavefront
+  // ---- in float64, all tokens of the wavefront; in LDS and in short loops (code that is seldom run is not in the instruction cache)
   if (__ballot(unsure)) {
-    double key[C];
-    if (how.sigmoid) {
-#pragma unroll
-      for (int c = 0; c < C; ++c) key[c] = 1.0 / (1.0 + exp(-(double)l[c]));
-    } else {
-      double sum = 0.0;
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        key[c] = l[c] == most ? 1.0 : l[c] > -INFINITY ? exp((double)l[c] - (double)most) : 0.0;
-        sum += key[c];
+    double* const scores = mine + n_experts;
+    double sum = 1.0;
+    if (!how.sigmoid) {
+      sum = 0.0;
+#pragma unroll 4
+      for (int e = lane; e < n_experts; e += L) {
+        const double v = to_float(row[e]);
+        mine[e] = v == (double)most ? 1.0 : v > -INFINITY ? exp(v - (double)most) : 0.0;
+        sum += mine[e];
       }
-      const double inverse = 1.0 / lanes_sum<L>(sum);
-#pragma unroll
-      for (int c = 0; c < C; ++c) key[c] *= inverse;
+      sum = lanes_sum<L>(sum);
     }
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      key[c] += (double)b[c];
-      if (!(l[c] > -INFINITY) || !(key[c] > -INFINITY)) key[c] = -INFINITY;
+    const double inverse = 1.0 / sum;
+#pragma unroll 4
+    for (int e = lane; e < n_experts; e += L) {
+      const double v = to_float(row[e]);
+      double key = how.sigmoid ? 1.0 / (1.0 + exp(-v)) : mine[e] * inverse;
+      if (how.bias) key += (double)how.bias[e];
+      mine[e] = v > -INFINITY && key > -INFINITY ? key : -INFINITY;
     }
+    lds_meet();
     if (grouped) {
-      double* scores = mine + n_experts;
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-        if (first + c < n_experts) mine[first + c] = key[c];
-      lds_meet();
       for (int g = lane; g < how.n_groups; g += L) {
         double best = -INFINITY, second = -INFINITY;
 #pragma unroll 8
@@ -249,27 +286,27 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
         scores[g] = how.group_top == 1 || second == -INFINITY ? best : best + second;
       }
       lds_meet();
-      bool close;
-      const unsigned long long stay = staying_groups<L>(scores, (double)-INFINITY, how.n_groups, how.top_groups, lane, base, -1.0, 0.0, &close);
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-        if (!(stay >> (int)(((float)(first + c) + 0.5f) * inverse_each) & 1)) key[c] = -INFINITY;
+      const unsigned long long stay = staying_groups<L, double>(scores, -INFINITY, how.n_groups, how.top_groups, lane, base, nullptr, nullptr);
+#pragma unroll 1
+      for (int e = lane; e < n_experts; e += L)
+        if (!(stay >> (int)(((float)e + 0.5f) * inverse_each) & 1)) mine[e] = -INFINITY;
+      lds_meet();
     }
     id = -1;
+#pragma unroll 1
     for (int j = 0; j < top_k; ++j) {
-      double best = key[0];
-      int at = 0;
-#pragma unroll
-      for (int c = 1; c < C; ++c)
-        if (key[c] > best) { best = key[c]; at = c; }
+      double best = -INFINITY;
+      int at = n_experts;
+#pragma unroll 8
+      for (int e = lane; e < n_experts; e += L)
+        if (mine[e] > best) { best = mine[e]; at = e; }
       const double top = lanes_max<L>(best);
-      const int owner = __ffsll(lanes_of<L>(__ballot(best == top), base)) - 1;
-      // (the owner's expert to all lanes, as a float: below 2^24)
-      const float e = lanes_max<L>(lane == owner ? (float)(first + at) : -1.f);
-      if (lane == j && top > -INFINITY) id = (int)e;
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-        if (lane == owner && c == at) key[c] = -INFINITY;
+      // (the lowest number of those with the largest, as a float: below 2^24)
+      const int lowest = (int)-lanes_max<L>(best == top ? -(float)at : -INFINITY);
+      if (top > -INFINITY) {
+        if (lane == j) id = lowest;
+        if (at == lowest) mine[at] = -INFINITY;
+      }
     }
   }
 
@@ -384,7 +421,7 @@ extern "C" sptir_status_t sptir_moe_route_groups(const void* logits, int32_t typ
     with_lanes(n_experts, top_k, [&](auto l, auto c) {
       constexpr int kLanes = decltype(l)::value;
       // (at most 16 tokens of 256 experts or 4 of 1024, and 64 groups: 40 KB)
-      const size_t lds = how.top_groups < how.n_groups ? sizeof(double) * (256 / kLanes) * (n_experts + how.n_groups) : 0;
+      const size_t lds = sizeof(double) * (256 / kLanes) * (n_experts + how.n_groups);
       in_launches(n_tokens, kLanes, [&](int64_t t, int32_t n, dim3 grid) {
         hipLaunchKernelGGL((k_moe_route_groups<T, kLanes, decltype(c)::value>), grid, dim3(256), lds, (hipStream_t)stream,
                            (const T*)logits + t * ld_logits, ld_logits, n, n_experts, top_k, how, experts + t * top_k, weights + t * top_k);
