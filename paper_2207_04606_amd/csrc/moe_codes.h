@@ -13,13 +13,11 @@ inline int64_t moe_blocks(int64_t width) { return (width + kMoeBlock - 1) / kMoe
 __device__ inline float code_unit(uint32_t exponent) {
   return exponent == 255 ? __builtin_nanf("") : __builtin_bit_cast(float, exponent << 23);
 }
-__device__ inline float code_of(uint32_t word, int byte) { return (float)(int8_t)(word >> 8 * byte); }
-
 // The first `many` of kN codes, zeros behind them
 template <int kN>
 struct Codes {
   uint32_t w[kN / 4];
-  __device__ inline float at(int i) const { return code_of(w[i / 4], i % 4); }
+  __device__ inline float at(int i) const { return (float)(int8_t)(w[i / 4] >> i % 4 * 8); }
 };
 template <int kN>
 __device__ inline Codes<kN> read_codes(const int8_t* p, int many) {

@@ -104,6 +104,10 @@ struct Eight {
   typename Mma<T>::Frag w[8 / kN];
   __device__ inline float at(int i) const { return to_float<T>(w[i / kN][i % kN]); }
 };
+struct EightValues {
+  float v[8];
+  __device__ inline float at(int i) const { return v[i]; }
+};
 template <typename T, bool kWords>
 __device__ inline Eight<T> read_8(const T* p, int32_t many) {
   using Word = typename Mma<T>::Frag;
@@ -140,17 +144,6 @@ __device__ inline void write_8(T* p, int32_t many, const float (&v)[8]) {
     }
   }
 }
-// ... of a row that is kept in 8 bits: as T they are what they stand for, exactly
-template <typename T, bool kOne>
-__device__ inline Eight<T> kept_8(const Kept<8, kOne>& kept) {
-  constexpr int kN = Eight<T>::kN;
-  Eight<T> e;
-  float v[8];
-  kept.values(v);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) e.w[i / kN][i % kN] = from_float<T>(v[i]);
-  return e;
-}
 template <int kAct, typename T>
 __device__ inline void act_8(float (&v)[8]) {
 #pragma unroll
@@ -173,10 +166,10 @@ __device__ inline void add_8(float (&v)[8], const Eight<T>& w) {
 enum MoeEnd { kEndNone, kEndAct, kEndSwiglu, kEndParts, kEndPartsSum };
 
 // Eight columns of a row of C from the sums: `bias` and `other` (forward: the residual; dx: z of the product before) have been
-// read by the caller, together for many rows.
-template <typename T, MoeOp kOp, MoeEnd kEnd, bool kWords>
+// read by the caller, together for many rows.  (Other: that of eight elements, or what eight values are that were kept in 8 bits.)
+template <typename T, MoeOp kOp, MoeEnd kEnd, bool kWords, typename Other = Eight<T>>
 __device__ inline void moe_emit_8(const MoeProduct& p, int32_t act, int expert, int64_t i, int32_t j, int32_t many, const float* acc,
-                                  const Eight<T>& bias, const Eight<T>& other, const Eight<T>& pair) {
+                                  const Eight<T>& bias, const Other& other, const Other& pair) {
   float v[8];
 #pragma unroll
   for (int x = 0; x < 8; ++x) v[x] = acc[x];

@@ -588,10 +588,13 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
               const int32_t j = my_j + x * 8;
               if (j >= out_cols) return;
               if constexpr (kKept) {
-                other[0][x] = kept_8<O, true>(kept[ff][x]);
-                if constexpr (kEnd == kEndSwiglu) pair[0][x] = kept_8<O, kPairOne>(kept_pair[ff][x]);
+                EightValues z, z_pair = {};
+                kept[ff][x].values(z.v);
+                if constexpr (kEnd == kEndSwiglu) kept_pair[ff][x].values(z_pair.v);
+                moe_emit_8<O, kOp, kEnd, kWords>(p, act, done.expert, i, j, out_cols - j, v + x * 8, bias[x], z, z_pair);
+              } else {
+                moe_emit_8<O, kOp, kEnd, kWords>(p, act, done.expert, i, j, out_cols - j, v + x * 8, bias[x], other[ff][x], pair[ff][x]);
               }
-              moe_emit_8<O, kOp, kEnd, kWords>(p, act, done.expert, i, j, out_cols - j, v + x * 8, bias[x], other[kKept ? 0 : (int)ff][x], pair[kKept ? 0 : (int)ff][x]);
             });
           }
         });
