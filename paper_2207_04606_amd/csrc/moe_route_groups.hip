@@ -43,6 +43,14 @@ __device__ inline int32_t marked_key(float v, int c) {
 }
 __device__ inline float of_key(int32_t cut) { return __builtin_bit_cast(float, cut ^ ((cut >> 31) & 0x7fffffff)); }
 
+// exp(x) within 2^-22 for |x| up to 80, which others are brought to (sigmoids of them are below kFloor, or 1): 2^(x / log 2) with what the
+// rounding of the exponent left.  A third of the instructions of a library's, which takes all x.
+__device__ inline float exp_near(float x) {
+  x = fminf(fmaxf(x, -80.f), 80.f);
+  const float hi = x * 1.44269504f, lo = fmaf(x, 1.44269504f, -hi) + x * 1.92596299e-8f, e = __builtin_amdgcn_exp2f(hi);
+  return fmaf(e, lo * 0.693147181f, e);
+}
+
 // The bits of a token's L lanes
 template <int L>
 __device__ inline unsigned long long lanes_of(unsigned long long ballot, int base) {
@@ -126,7 +134,7 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
     float key[C], size = 0.f;
     if (how.sigmoid) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) key[c] = __builtin_amdgcn_rcpf(1.f + expf(-l[c]));
+      for (int c = 0; c < C; ++c) key[c] = __builtin_amdgcn_rcpf(1.f + exp_near(-l[c]));
     } else {
       double sum = 0.0;
 #pragma unroll
@@ -180,7 +188,7 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
       float gap, size_of_both;
       const unsigned long long stay = staying_groups<L>(scores, -kFar, how.n_groups, how.top_groups, lane, base, &gap, &size_of_both);
       // (A score is a sum of two, which may cancel: the larger is at most 1 + the largest bias B, the other's size no more than that and the score's.  So of
-      // two scores, each of two sigmoids within 2^-21.9 and three roundings of sums, the distance is within 2^-19.9 + 2^-22 (1 + B) + 2^-22 of the larger; softmaxes 2^-21.)
+      // two scores, each of two sigmoids within 2^-21.7 and three roundings of sums, the distance is within 2^-19.7 + 2^-22 (1 + B) + 2^-22 of the larger; softmaxes 2^-21.)
       const float apart = how.bias ? (how.sigmoid ? 0x1p-19f : 0x1p-18f) * (1.f + fmaxf(lanes_max<L>(size), 0.f)) + 0x1p-21f * size_of_both : 0x1p-16f * size_of_both;
       unsure = unsure || !(gap > apart);
 #pragma unroll

@@ -89,6 +89,7 @@ __device__ inline uint32_t turned_bits(uint32_t v) { return __builtin_amdgcn_upd
 
 // Rounding by an addition: 1.5 * 2^23 + a number below 2^22 is rounded to a whole number, to even, whose two's complement has the low bits.
 constexpr float kRound = 12582912.f;
+constexpr float kSure = 0.5f - 0x1p-15f;  // as near the middle as a guess may be
 
 // The whole number nearest to x / s, the even one of two: a guess, one off at most, and what it leaves, which is exact.  (With u the unit of s's
 // last place, x and the guess times s are multiples of u / 2; what is left, up to s / 2, is below 2^24 of them, and where it is more
@@ -103,8 +104,8 @@ __device__ inline int nearest(float x, float s, float inverse) {
 }
 
 // A group of lanes per row: the largest magnitude, then the codes, for which the row comes from the caches.  An element's code is x times the reciprocal
-// of the scale, rounded: within 2^-16 of the quotient, so the nearest one wherever that is not next to the middle of two; a word with such a one (of 512
-// elements 1 in 30) is done with care.  (Rows held in registers between the two made the code five times as long: 16,384 x 4096 of bf16 73 us, now 56.)
+// of the scale, rounded: within 2^-16 of the quotient, so the nearest one wherever that is not next to the middle of two; such elements are done with care.  (Of float32's one in 2^14; of
+// those of 16 bits all that are half of the row's largest, which is next to the middle between 63 and 64: somewhere in most words.)  (Rows held in registers between the two made the code five times as long: 16,384 x 4096 of bf16 73 us, now 56.)
 template <typename T>
 __global__ __launch_bounds__(256) void k_moe_quantise(Rows8 p) {
   constexpr int kN = Word<T>::kN;
@@ -151,9 +152,13 @@ __global__ __launch_bounds__(256) void k_moe_quantise(Rows8 p) {
         q[i] = __builtin_bit_cast(uint32_t, sum);
         near = fmaxf(near, fabsf(fmaf(v, inverse, kRound - sum)));
       }
-      if (!(near < 0.5f - 0x1p-15f) || careful) {
+      if (!(near < kSure) || careful) {
 #pragma unroll
-        for (int i = 0; i < kN; ++i) q[i] = inverse > 0.f ? (uint32_t)nearest(w.at(i) * up, su, inverse) : 0u;
+        for (int i = 0; i < kN; ++i) {
+          const float v = w.at(i);
+          if (__builtin_expect(careful || !(fabsf(fmaf(v, inverse, kRound - __builtin_bit_cast(float, q[i]))) < kSure), 0))
+            q[i] = inverse > 0.f ? (uint32_t)nearest(v * up, su, inverse) : 0u;
+        }
       }
       write_codes<kN>(p.Q + r * p.ldq + c, p.width - c, q);
     }

@@ -146,6 +146,21 @@ def test_no_inputs(gpu_lib):
         assert torch.equal(Y, bias.expand(rows, 24))
 
 
+@pytest.mark.parametrize("rows", [6, 900])
+def test_experts_that_share_weights(gpu_lib, rows):
+    """W and its scales of stride 0: one matrix for all experts."""
+    gen = torch.Generator().manual_seed(rows)
+    e = torch.randint(0, 5, (rows, 1), generator=gen, dtype=torch.int32)
+    r = gpu_lib.sptir_moe_sort(e.cuda(), 5)
+    X = torch.randint(-127, 128, (rows, 96), generator=gen, dtype=torch.int8)
+    W, ws, xs = torch.randint(-127, 128, (1, 40, 96), generator=gen, dtype=torch.int8), torch.rand(1, 40, generator=gen), torch.rand(rows, generator=gen)
+    Y = torch.empty(rows, 40, device="cuda")
+    gpu_lib.sptir_moe_product_int8(r, X.cuda(), xs.cuda(), W.cuda().expand(5, 40, 96), ws.cuda().expand(5, 40), Y, gather=True)
+    at = r.entry_of.cpu().long()
+    want = (X[at].double() @ W[0].double().t()) * xs[at].double()[:, None] * ws[0].double()
+    ref.check(Y, want, want.abs() * 2.0 ** -22 + 2.0 ** -126, "y")
+
+
 def test_in_a_graph_and_on_streams(gpu_lib):
     """Quantise and product, captured together and replayed with new inputs, and on another stream, give the bits of eager calls."""
     T, k, E, K, N = 300, 2, 6, 256, 192

@@ -141,6 +141,60 @@ def test_gradient_against_differences(gpu_lib, scores, normalise):
     assert ((slope - want).abs() <= limit).all()
 
 
+def test_more_tokens_than_a_launch_takes(gpu_lib):
+    """2^25 tokens and a few: the last ones and those at the border."""
+    T, E, k = (1 << 25) + 5, 4, 2
+    l = torch.empty(T, E, dtype=torch.bfloat16, device="cuda").normal_()
+    bias = torch.tensor([0.1, -0.1, 0.3, 0.0], device="cuda")
+    experts = torch.full((T, k), -7, dtype=torch.int32, device="cuda")
+    weights = torch.full((T, k), math.nan, device="cuda")
+    how = {"scores": "sigmoid", "n_groups": 2, "top_groups": 1, "group_top": 2}
+    gpu_lib.sptir_moe_route_groups(l, experts, weights, bias=bias, **how)
+    assert int(experts.amin()) >= 0 and bool(torch.isfinite(weights).all())
+    d = torch.full((T, E), math.nan, dtype=torch.bfloat16, device="cuda")
+    gpu_lib.sptir_moe_route_groups_backward(l, experts, weights, torch.ones_like(weights), d, scores="sigmoid")
+    assert bool(torch.isfinite(d).all())
+    for at in (slice(0, 64), slice((1 << 25) - 32, T)):
+        want, w_want = ref8.route(l[at].cpu(), k, bias=bias.cpu(), normalise=True, scale=1.0, **how)
+        assert torch.equal(experts[at].cpu(), want)
+        ref.check(weights[at], w_want, w_want * 2.0 ** -23, "weights")
+
+
+@pytest.mark.parametrize("scores", ["sigmoid", "softmax"])
+def test_in_a_graph(gpu_lib, scores):
+    T, E, k = 300, 64, 4
+    gen = torch.Generator().manual_seed(8)
+    inputs = [randn(gen, T, E).cuda() for _ in range(3)]
+    bias, dw = (0.1 * randn(gen, E)).cuda(), randn(gen, T, k).cuda()
+    l, d = inputs[0].clone(), torch.empty(T, E, device="cuda")
+    experts, weights = torch.empty(T, k, dtype=torch.int32, device="cuda"), torch.empty(T, k, device="cuda")
+
+    def step(stream=None):
+        gpu_lib.sptir_moe_route_groups(l, experts, weights, scores=scores, bias=bias, n_groups=8, top_groups=3, group_top=2, stream=stream)
+        gpu_lib.sptir_moe_route_groups_backward(l, experts, weights, dw, d, scores=scores, stream=stream)
+
+    want = []
+    for x in inputs:
+        l.copy_(x)
+        step()
+        want.append([t.clone() for t in (experts, weights, d)])
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for n in range(6):
+        l.copy_(inputs[n % 3])
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip((experts, weights, d), want[n % 3]))
+        inputs[0].sum().item()
+        d.fill_(math.nan)
+        side.wait_stream(torch.cuda.current_stream())
+        step(side)
+        torch.cuda.current_stream().wait_stream(side)
+        assert all(torch.equal(a, b) for a, b in zip((experts, weights, d), want[n % 3]))
+
+
 def test_refusals(gpu_lib):
     l = torch.zeros(4, 12, device="cuda")
     e, w = torch.empty(4, 2, dtype=torch.int32, device="cuda"), torch.empty(4, 2, device="cuda")

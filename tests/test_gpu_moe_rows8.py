@@ -147,6 +147,20 @@ def test_pack_at_the_ends(gpu_lib, dtype):
     assert torch.equal(got[:9], values[:9])
 
 
+@pytest.mark.parametrize("n,width", [(700001, 8), (70001, 300)])
+def test_more_rows_than_workgroups(gpu_lib, n, width):
+    X = randn(torch.Generator().manual_seed(n), n, width, dtype=BF16)
+    Q, E = packed(gpu_lib, X)
+    want, e_want = ref8.pack(X)
+    assert torch.equal(E.cpu(), e_want) and torch.equal(Q.cpu(), want)
+    out, s = torch.empty(n, width, dtype=BF16, device="cuda"), torch.empty(n, device="cuda")
+    gpu_lib.sptir_moe_unpack(Q, E, out)
+    assert torch.equal(out.cpu(), ref8.kept(want, e_want, BF16))
+    gpu_lib.sptir_moe_quantise(X.cuda(), Q, s)
+    want, s_want = ref8.quantise(X)
+    assert torch.equal(Q.cpu(), want) and torch.equal(s.cpu(), s_want)
+
+
 def test_large_strides(gpu_lib):
     """Rows whose places pass 2^32 bytes."""
     n, width, ld = 3, 40, 1 << 31
