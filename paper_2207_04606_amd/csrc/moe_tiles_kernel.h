@@ -167,7 +167,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
     uint32_t dealt = moe_deal(id, total);
     int jt;
     if constexpr (kOp == kMoeDw) {
-      if (order && id / gridDim.x % 2) {  // (every other turn the other way round: a workgroup with a long one has a short one next)
+      if (order && id >= gridDim.x) {  // (all turns but the first the other way round: the longest tiles' workgroups have the shortest ones then)
         const uint32_t first = id - blockIdx.x;
         dealt = first + min(first + gridDim.x, total) - 1 - dealt;
       }
