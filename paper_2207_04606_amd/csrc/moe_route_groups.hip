@@ -58,9 +58,10 @@ __device__ inline unsigned long long lanes_of(unsigned long long ballot, int bas
   return L == 64 ? mine : mine & 0xffff;
 }
 
-// The groups that stay, as bits, from their scores in LDS; *gap: how much less the best of the others has than the last of them, *size: the larger magnitude of both.
+// The groups that stay, as bits, from their scores in LDS; *gap: how much less the best of the others has than the last of them, *size: the larger magnitude of both; *last: that
+// of the last of them.
 template <int L, typename V>
-__device__ inline unsigned long long staying_groups(const V* scores, V none, int n_groups, int top_groups, int lane, int base, V* gap, V* size) {
+__device__ inline unsigned long long staying_groups(const V* scores, V none, int n_groups, int top_groups, int lane, int base, V* gap, V* size, V* last) {
   unsigned long long stay = 0;
   V lowest = (V)INFINITY, highest = none;
   for (int g0 = 0; g0 < n_groups; g0 += L) {
@@ -86,6 +87,7 @@ __device__ inline unsigned long long staying_groups(const V* scores, V none, int
     highest = lanes_max<L>(highest);
     *gap = highest == none ? (V)INFINITY : lowest - highest;
     *size = fabs(lowest) > fabs(highest) ? fabs(lowest) : fabs(highest);
+    *last = lowest;
   }
   return stay;
 }
@@ -157,6 +159,17 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
       size = fmaxf(size, b[c]);
       key[c] = !there ? -kFar : fminf(fmaxf(v, how.bias ? -kMost : kFloor), kMost);
     }
+    const bool logit_keys = sizeof(T) == 2 && !how.bias, sums = how.group_top == 2;
+    auto take_logits = [&] {
+#pragma unroll
+      for (int c = 0; c < C; ++c) key[c] = key[c] == -kFar ? -kFar : fminf(fmaxf(l[c], -kMost), kMost);
+    };
+    // whether float64 may not tell the score of such a key from that of one `gap` below
+    auto unclear = [&](float logit, float gap) {
+      const float exponent = how.sigmoid ? logit : logit - most;
+      return !(fabsf(exponent) < 600.f) || (how.sigmoid && logit > 30.f) || (gap != 0.f && gap < 0x1p-40f);
+    };
+    if (logit_keys && !sums) take_logits();
     if (grouped) {
       float* scores = (float*)mine;
       float best = -kFar, second = -kFar;
@@ -185,21 +198,18 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
         }
         lds_meet();
       }
-      float gap, size_of_both;
-      const unsigned long long stay = staying_groups<L>(scores, -kFar, how.n_groups, how.top_groups, lane, base, &gap, &size_of_both);
+      float gap, size_of_both, lowest;
+      const unsigned long long stay = staying_groups<L>(scores, -kFar, how.n_groups, how.top_groups, lane, base, &gap, &size_of_both, &lowest);
       // (A score is a sum of two, which may cancel: the larger is at most 1 + the largest bias B, the other's size no more than that and the score's.  So of
       // two scores, each of two sigmoids within 2^-21.7 and three roundings of sums, the distance is within 2^-19.7 + 2^-22 (1 + B) + 2^-22 of the larger; softmaxes 2^-21.)
       const float apart = how.bias ? (how.sigmoid ? 0x1p-19f : 0x1p-18f) * (1.f + fmaxf(lanes_max<L>(size), 0.f)) + 0x1p-21f * size_of_both : 0x1p-16f * size_of_both;
-      unsure = unsure || !(gap > apart);
+      if (logit_keys && !sums) unsure = unsure || (gap < INFINITY && unclear(lowest, gap));
+      else unsure = unsure || !(gap > apart);
 #pragma unroll
       for (int c = 0; c < C; ++c)
         if (!(stay >> (int)(((float)(first + c) + 0.5f) * inverse_each) & 1)) key[c] = -kFar;
     }
-    const bool logit_keys = sizeof(T) == 2 && !how.bias;
-    if (logit_keys) {
-#pragma unroll
-      for (int c = 0; c < C; ++c) key[c] = key[c] == -kFar ? -kFar : fminf(fmaxf(l[c], -kMost), kMost);
-    }
+    if (logit_keys && sums) take_logits();
     int32_t order[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) order[c] = marked_key<C>(key[c], c);
@@ -218,8 +228,7 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
       const bool some = top > -0.5f * kFar;
       bool apart = j > 0;
       if (some && logit_keys) {
-        const float exponent = how.sigmoid ? top : top - most;
-        unsure = unsure || (more && (!(fabsf(exponent) < 600.f) || (how.sigmoid && top > 30.f) || (j > 0 && top != last && last - top < 0x1p-40f)));
+        unsure = unsure || (more && unclear(top, j > 0 ? last - top : 0.f));
       } else if (some) {
         const float larger = fmaxf(fabsf(last), fabsf(top));
         unsure = unsure || (more && larger > 0x1p80f);
@@ -294,7 +303,7 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
         scores[g] = how.group_top == 1 || second == -INFINITY ? best : best + second;
       }
       lds_meet();
-      const unsigned long long stay = staying_groups<L, double>(scores, -INFINITY, how.n_groups, how.top_groups, lane, base, nullptr, nullptr);
+      const unsigned long long stay = staying_groups<L, double>(scores, -INFINITY, how.n_groups, how.top_groups, lane, base, nullptr, nullptr, nullptr);
 #pragma unroll 1
       for (int e = lane; e < n_experts; e += L)
         if (!(stay >> (int)(((float)e + 0.5f) * inverse_each) & 1)) mine[e] = -INFINITY;
