@@ -1,17 +1,19 @@
 // The experts' products in tiles: operands from memory to LDS, matrix instructions from there.  (Compiled once for every
-// product, moe_tiles_forward.hip, moe_tiles_dx.hip and moe_tiles_dw.hip.)
+// product, moe_tiles_forward.hip, moe_tiles_dx.hip, moe_tiles_dw.hip, moe_tiles_int8.hip and moe_tiles_dx_kept.hip.)
 //
 // A workgroup keeps a tile of C in registers and adds up 128 bytes of r a step.  A step of a wide tile is 2048 clocks of matrix
 // instructions beside 768 of LDS, by its counter: eight wavefronts read (128 + 64) x 128 bytes each for 2^15 x 64 multiply-adds.  What bounds
 // it are the waits: of a CU's clocks matrix instructions fill 52 to 56 % (8192 x 4096 x 4096; 8192 x 8192 rows of prompts), a wavefront waits a third
 // of its time, at the step's barrier and for its reads.
-// With long rows 8192 x 8192 x 8192 of bf16 take 900 us, 1220 TFLOP/s (a large library product reaches 1290), 8192 x 4096 x 4096
-// 250 us, 1100, the gradients 1070 and 1030.  With short ones (r = 1024) the step's loads are not there in time, since all
-// workgroups ask memory for new operands at once, and the epilogue is a sixth of the tile: 32,768 rows, 1024 x 2048, 140 us, 980.
-// The gradients of 16 bits (39, 30 and 31 % matrix instructions in forward, dX and dW of those sizes with uneven experts) lose more: the compiler takes
-// the transposing LDS reads to need the loads that write LDS and waits for all of these before the first such read of a step (dW) or of its
-// second half (dX), so that a step's loads have a part of a step to arrive in, not a whole one; 4 to 8 % of the clocks are LDS bank conflicts; and the wide
-// kernels spill at the change of tile (dW 20 registers, 28 with db; dX 10 to 16), where every reload waits for all loads too.
+// With long rows 8192 x 8192 x 8192 of bf16 take 840 us, 1310 TFLOP/s (a large library product reaches 1380), 8192 x 4096 x 4096
+// 237 us, 1160, the gradients 1220 and 1270; of 8-bit integers 440 us, 2500 TOP/s (the library's 2050), and 144 us, 1910.  With short
+// ones (r = 1024) the step's loads are not there in time, since all workgroups ask memory for new operands at once, and the epilogue is a sixth of the tile:
+// 32,768 rows, 1024 x 2048, 140 us, 980.
+// The gradients of 16 bits lose more where experts have different rows (32,768 rows of 32 experts, 2048 x 1024: dX 188 us, dW 187, 730 TFLOP/s; matrix instructions fill
+// 34 % of a CU's clocks in dW): tiles of 600 to 3000 rows do not come out even over four turns (a sixth of dW by the rows' numbers); 4 to 8 % of the clocks are
+// LDS bank conflicts; and the wide kernels spill at the change of tile (dW 10 registers, 22 with db; dX 10 to 16), where every reload waits for all loads too.
+// The derivative of an activation is arithmetic that no matrix instructions run beside, unless the CU's other workgroup has some: 11 us of a narrow tile with
+// gelu (8192 x 1024 x 4096: 73 us without, 84 with it), whether z has 16 bits or 8.
 // float32 is bound by its instructions: 4096 x 4096 x 4096 1040 us, 132 TFLOP/s (a library product: 150).  Operands that do not
 // lie in words pass through registers: 540 TFLOP/s in 16 bits.  Measured and left out: tiles of 64 x 64 and 64 x 128 (not faster
 // where the others are few, 1.5 times slower where many), four steps in LDS for a workgroup alone on its CU (no faster: it waits for
@@ -408,8 +410,9 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   };
 
   // One step.  The barrier before its last phase says that this step's part of LDS has been read and that the next step's is
-  // there.  The order of a phase is kept as it is written
-  // (fences): reads first, so that they arrive while the phase's matrix instructions run.
+  // there.  The order of a phase is kept as it is written (fences): a first matrix instruction, the next phase's reads, which arrive
+  // while the others run.  (The compiler waits for all reads that are under way, not for those that are needed, while loads to LDS
+  // are: with the reads first, it waited for those just asked for.  8192 x 2048 x 8192 of 8-bit integers 324 -> 305 us, dW 199 -> 190.)
   using Set0 = std::integral_constant<int, 0>;
   // A whole tile's epilogue issues at least so many stores behind the next tile's first loads: these need not be waited for
   // with the loads.
