@@ -118,7 +118,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_moe_few(MoeProduct p, int32_t a
   const bool none = t.expert == p.n_experts;
   Acc acc[kFM][kFN] = {};
   // The scales of the four columns of a row (gated: and their pairs) that this thread has in the end, asked for before the products:
-  // their memory's latency is that of x (8 experts' 2048 x 2048 bytes for one token 10.2 -> 9.0 us).
+  // their memory's latency is that of x (8 experts' 2048 x 2048 bytes for one token 10.2 -> 9.6 us).  (W asked for before the entries that say which rows
+  // of x there are have come: more registers, 4 tokens 26 -> 32 us.)
   constexpr int kPieces = kGated ? kFM : kFM * kFN;
   static_assert(kPieces * 64 <= kMoeFewThreads, "a piece of a thread");
   float of_row = 0.f, of_column[kGated ? 2 : 1][4] = {};
@@ -168,7 +169,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_moe_few(MoeProduct p, int32_t a
     int64_t r = wave * kStep;
     for (; r + (kTurns - 1) * kWaves * kStep + kStep <= p.n_r; r += kTurns * kWaves * kStep)
       turns(r, std::integral_constant<int, kTurns>{}, std::true_type{});
-    if (kTurns > 2)  // (of 2048 8-bit integers or 1024 of 16 bits a wavefront has two turns: 8 experts' 2048 x 2048 bytes for one token 10.4 -> 8.9 us)
+    if (kTurns > 2)  // (of 2048 8-bit integers or 1024 of 16 bits a wavefront has two turns: 8 experts' 2048 x 2048 bytes for one token 10.4 -> 10.2 us)
       for (; r + kWaves * kStep + kStep <= p.n_r; r += 2 * kWaves * kStep) turns(r, std::integral_constant<int, 2>{}, std::true_type{});
     if (kTurns > 1)
       for (; r + kStep <= p.n_r; r += kWaves * kStep) turns(r, std::integral_constant<int, 1>{}, std::true_type{});

@@ -98,7 +98,9 @@ __device__ inline void take_two(V v, V& best, V& second) {
   best = v > best ? v : best;
 }
 
-// L lanes per token, lane l has the experts l * C .. l * C + C - 1 (as k_moe_route).
+// L lanes per token, lane l has the experts l * C .. l * C + C - 1 (as k_moe_route).  Bound by instructions: k + 1 rounds over the C keys of a lane, and
+// by the slowest wavefront, one that chooses in float64 (an eighth of the time).  16,384 tokens of 256 experts: 8 groups 19 us, no groups 15; the logits'
+// bytes alone 3.5.  (All in float64: 33.)
 template <typename T, int L, int C>
 __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ logits, int64_t ld, int32_t n_tokens, int32_t n_experts,
                                                           int32_t top_k, Scoring how, int32_t* __restrict__ experts,
@@ -347,6 +349,7 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
 // With p = w / scale and m = sum w dw over the choices:
 //   softmax, normalised   dl = w (dw - m / scale) of a choice, others 0;   not   w dw - p m, others -p m, p of all experts
 //   sigmoid, normalised   dl = w (dw - m / scale) (1 - s);                 not   w dw (1 - s)
+// Bound by memory: 16,384 tokens of 256 experts of float32 5.9 us, 33.6 MB of logits and gradients (the logits from the memory-side cache).
 template <typename T, int L, int C>
 __global__ __launch_bounds__(256) void k_moe_route_groups_backward(const T* __restrict__ logits, int64_t ld, int32_t n_tokens,
                                                                    int32_t n_experts, int32_t top_k, Scoring how,
