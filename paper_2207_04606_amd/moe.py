@@ -454,11 +454,11 @@ def sptir_moe_quantise(X, Q, scales, stream=None) -> None:
     if X.dim() == 3 and isinstance(Q, torch.Tensor) and Q.dim() == 3 and isinstance(scales, torch.Tensor) and scales.dim() == 2:
         if Q.shape != X.shape or scales.shape != X.shape[:2]:
             raise ValueError(f"Q must be {list(X.shape)} and scales {list(X.shape[:2])}")
-        for t in (X, Q):
+        for t in (X, Q, scales):
             if not t.is_contiguous():
-                raise ValueError("the matrices of experts must be contiguous")
-        _dev(scales, torch.float32, "scales")
-        X, Q, scales = X.view(-1, X.shape[2]), Q.view(-1, Q.shape[2]), scales.view(-1)
+                raise ValueError("the matrices of experts and their scales must be contiguous")
+        rows = X.shape[0] * X.shape[1]
+        X, Q, scales = X.view(rows, X.shape[2]), Q.view(rows, X.shape[2]), scales.view(rows)
     if X.dim() != 2:
         raise ValueError("X must be [rows, width], or [E, rows, width] beside Q of the same shape")
     rows, width = X.shape

@@ -193,6 +193,18 @@ def test_nothing_to_do(gpu_lib):
         gpu_lib.sptir_moe_unpack(Q, E, X)
 
 
+def test_weights_without_columns_and_strided_scales(gpu_lib):
+    for E, n, width in ((3, 5, 0), (0, 5, 8), (3, 0, 8)):
+        s = torch.full((E, n), math.nan, device="cuda")
+        gpu_lib.sptir_moe_quantise(torch.empty(E, n, width, device="cuda"), torch.empty(E, n, width, dtype=torch.int8, device="cuda"), s)
+        assert (s == 0).all()
+    W, Q = torch.zeros(3, 5, 8, device="cuda"), torch.zeros(3, 5, 8, dtype=torch.int8, device="cuda")
+    with pytest.raises(ValueError):
+        gpu_lib.sptir_moe_quantise(W, Q, torch.zeros(3, 6, device="cuda")[:, :5])
+    with pytest.raises(ValueError):
+        gpu_lib.sptir_moe_quantise(W.mT, Q.mT, torch.zeros(3, 8, device="cuda"))
+
+
 def test_refusals(gpu_lib):
     X = torch.zeros(4, 64, device="cuda")
     Q, E, s = torch.zeros(4, 64, dtype=torch.int8, device="cuda"), torch.zeros(4, 2, dtype=torch.uint8, device="cuda"), torch.zeros(4, device="cuda")
