@@ -205,10 +205,13 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
       // (A score is a sum of two, which may cancel: the larger is at most 1 + the largest bias B, the other's size no more than that and the score's.  So of
       // two scores, each of two sigmoids within 2^-21.7 and three roundings of sums, the distance is within 2^-19.7 + 2^-22 (1 + B) + 2^-22 of the larger; softmaxes 2^-21.)
       // Without a bias what kFloor adds to the two of a score is up to 2^-99 more.
-      const float apart = how.bias ? (how.sigmoid ? 0x1p-19f : 0x1p-18f) * (1.f + fmaxf(lanes_max<L>(size), 0.f)) + 0x1p-21f * size_of_both
+      const float most_bias = fmaxf(lanes_max<L>(size), 0.f);
+      const float apart = how.bias ? (how.sigmoid ? 0x1p-19f : 0x1p-18f) * (1.f + most_bias) + 0x1p-21f * size_of_both
                                    : 0x1p-16f * size_of_both + (sums ? 0x1p-98f : 0.f);
       if (logit_keys && !sums) unsure = unsure || (gap < INFINITY && unclear(lowest, gap));
-      else unsure = unsure || !(gap > apart);
+      // (Below 2^80 no key that is cut off at 2^90 is part of the last group that stays, nor, cut off from above, of any; of another one it may be, from
+      // below: such a group is less than the others as it is.)
+      else unsure = unsure || !(gap > apart) || !(fmaxf(fabsf(lowest), most_bias) < 0x1p80f);
 #pragma unroll
       for (int c = 0; c < C; ++c)
         if (!(stay >> (int)(((float)(first + c) + 0.5f) * inverse_each) & 1)) key[c] = -kFar;

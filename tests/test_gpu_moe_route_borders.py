@@ -51,3 +51,21 @@ def test_one_small_score_beside_two(gpu_lib, scores):
     if scores == "sigmoid":
         l[0, :2] = -98.0 * ln2
     same(gpu_lib, l, 3, scores=scores, n_groups=4, top_groups=2, group_top=2)
+
+
+@pytest.mark.parametrize("scores", ["sigmoid", "softmax"])
+def test_groups_of_biases_past_the_keys(gpu_lib, scores):
+    """Biases beyond 2^90, where float32's keys are cut off, in sums with others: 2^91.5 - 2^91 is more than 2^75."""
+    big, off = [2.0 ** 91.5, -2.0 ** 91.0], -2.0 ** 100
+    cases = [([2.0 ** 75, 0.0, *big, 0.0, 0.0], 3, 1, 1), ([2.0 ** 70, 0.0, 2.0 ** 79.9, -2.0 ** 95, 0.0, -2.0 ** 90 * (1 - 2.0 ** -12), off, off], 4, 2, 1),
+             ([0.0, off, 0.1, 2 * off, 0.2, 4 * off, -0.1, off], 4, 2, 2), ([0.5, -3e38, 0.25, -3e38, 0.0, 0.0, 1e30, -1e31], 4, 2, 2),
+             ([2.0 ** 80, 2.0 ** 79, 2.0 ** 80, 2.0 ** 79.5, -2.0 ** 88, 2.0 ** 81, 1.0, 1.0], 4, 2, 2)]
+    gen = torch.Generator().manual_seed(7)
+    for bias, n_groups, top_groups, k in cases:
+        bias = torch.tensor(bias)
+        l = torch.cat([torch.zeros(1, len(bias)), randn(gen, 20, len(bias))])
+        same(gpu_lib, l, k, bias=bias, scores=scores, n_groups=n_groups, top_groups=top_groups, group_top=2)
+    for each in (2, 3, 8):
+        bias = torch.sign(randn(gen, 8 * each)) * torch.exp2(60.0 + 60.0 * torch.rand(8 * each, generator=gen))
+        bias[torch.rand(8 * each, generator=gen) < 0.5] = 0.0
+        same(gpu_lib, randn(gen, 50, 8 * each), 2, bias=bias, scores=scores, n_groups=8, top_groups=3, group_top=2)
