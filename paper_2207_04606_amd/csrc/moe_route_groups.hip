@@ -29,10 +29,12 @@ struct Scoring {
 // keys that are further apart than 2^-16 of the larger one, or with a bias than 2^-17 (1 + the larger one), say how c lie.  Tokens with two choices
 // closer than that (of 256 experts one in a hundred) are put in order by float64; those whose groups are, or whose keys float32 has no room for, are chosen from in float64
 // altogether, with the other tokens of the wavefront.
-// Logits of 16 bits without a bias are keys themselves, and ties are ties: a mark takes nothing from them.  Float64 tells their scores
-// apart while exponents are within +- 600, sigmoids' logits below 30 and differences not below 2^-40.
+// Logits of 16 bits without a bias are keys themselves, and ties are ties: a mark takes nothing from them, and both zeros are one.  Float64 tells their scores
+// apart while exponents are within +- 600, sigmoids' logits below 30 and differences not below 2^-40.  Of equal ones, which their type's step (2^-11 of them at
+// least) keeps that far from the next, that holds down to 2^-28; of smaller ones where no logit but zero is as small.
 constexpr float kFar = 0x1p100f;  // past all keys
 constexpr float kMost = 0x1p90f;  // keys are cut off here, and a choice past 2^80 is left to float64
+constexpr float kSmall = 0x1p-28f;
 constexpr float kFloor = 0x1p-100f;  // of scores without a bias: those that are smaller are alike here
 // A float32 as a whole number with the same order, its last four bits for the mark, and back without it
 template <int C>
@@ -164,7 +166,7 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
     const bool logit_keys = sizeof(T) == 2 && !how.bias, sums = how.group_top == 2;
     auto take_logits = [&] {
 #pragma unroll
-      for (int c = 0; c < C; ++c) key[c] = key[c] == -kFar ? -kFar : fminf(fmaxf(l[c], -kMost), kMost);
+      for (int c = 0; c < C; ++c) key[c] = key[c] == -kFar ? -kFar : fminf(fmaxf(l[c] + 0.f, -kMost), kMost);  // (-0 + 0 is 0)
     };
     // whether float64 may not tell the score of such a key from that of one `gap` below
     auto unclear = [&](float logit, float gap) {
@@ -172,6 +174,7 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
       return !(fabsf(exponent) < 600.f) || (how.sigmoid && logit > 30.f) || (gap != 0.f && gap < 0x1p-40f);
     };
     if (logit_keys && !sums) take_logits();
+    bool small = false;  // what is chosen ends among equal logits below kSmall
     if (grouped) {
       float* scores = (float*)mine;
       float best = -kFar, second = -kFar;
@@ -208,10 +211,14 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
       const float most_bias = fmaxf(lanes_max<L>(size), 0.f);
       const float apart = how.bias ? (how.sigmoid ? 0x1p-19f : 0x1p-18f) * (1.f + most_bias) + 0x1p-21f * size_of_both
                                    : 0x1p-16f * size_of_both + (sums ? 0x1p-98f : 0.f);
-      if (logit_keys && !sums) unsure = unsure || (gap < INFINITY && unclear(lowest, gap));
-      // (Below 2^80 no key that is cut off at 2^90 is part of the last group that stays, nor, cut off from above, of any; of another one it may be, from
-      // below: such a group is less than the others as it is.)
-      else unsure = unsure || !(gap > apart) || !(fmaxf(fabsf(lowest), most_bias) < 0x1p80f);
+      if (logit_keys && !sums) {
+        unsure = unsure || (gap < INFINITY && unclear(lowest, gap));
+        small = gap == 0.f && fabsf(lowest) < kSmall;
+      } else {
+        // (Below 2^80 no key that is cut off at 2^90 is part of the last group that stays, nor, cut off from above, of any; of another one it may be,
+        // from below: such a group is less than the others as it is.)
+        unsure = unsure || !(gap > apart) || !(fmaxf(fabsf(lowest), most_bias) < 0x1p80f);
+      }
 #pragma unroll
       for (int c = 0; c < C; ++c)
         if (!(stay >> (int)(((float)(first + c) + 0.5f) * inverse_each) & 1)) key[c] = -kFar;
@@ -236,6 +243,7 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
       bool apart = j > 0;
       if (some && logit_keys) {
         unsure = unsure || (more && unclear(top, j > 0 ? last - top : 0.f));
+        small = small || (more && j >= top_k && last == top && fabsf(top) < kSmall);
       } else if (some) {
         const float larger = fmaxf(fabsf(last), fabsf(top));
         unsure = unsure || (more && larger > 0x1p80f);
@@ -256,6 +264,18 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
       const int32_t taken = lane == owner ? best : INT32_MIN;
 #pragma unroll
       for (int c = 0; c < C; ++c) order[c] = order[c] == taken ? INT32_MIN : order[c];
+    }
+    // (Float16 has no logit but zero that is as small.)
+    if constexpr (std::is_same_v<T, __bf16>) {
+      if (__ballot(small)) {
+        float again[C];
+        read_logits<T, C>(row, first, n_experts, again);
+        bool other = false;
+#pragma unroll
+        for (int c = 0; c < C; ++c) other = other || (again[c] != 0.f && fabsf(again[c]) < kSmall);
+        const bool others = lanes_of<L>(__ballot(other), base) != 0;
+        unsure = unsure || (small && others);
+      }
     }
     // Those that are close are put in order by what they are in float64 (without a bias softmaxes by their exponentials).
     unsure = unsure || (tight && !how.sigmoid && how.bias);

@@ -69,3 +69,55 @@ def test_groups_of_biases_past_the_keys(gpu_lib, scores):
         bias = torch.sign(randn(gen, 8 * each)) * torch.exp2(60.0 + 60.0 * torch.rand(8 * each, generator=gen))
         bias[torch.rand(8 * each, generator=gen) < 0.5] = 0.0
         same(gpu_lib, randn(gen, 50, 8 * each), 2, bias=bias, scores=scores, n_groups=8, top_groups=3, group_top=2)
+
+
+# ------------------------------------------------------------------------------------------------ 16-bit logits as keys
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("n_groups,top_groups,group_top", GROUPS)
+def test_sigmoids_next_to_one(gpu_lib, dtype, n_groups, top_groups, group_top):
+    """Past 37 all sigmoids are 1 in float64, and ties go to the lower id, where the larger logits have the higher ones."""
+    gen = torch.Generator().manual_seed(n_groups + group_top)
+    T, E = 200, 64
+    l = torch.sort(28.0 + 32.0 * torch.rand(T, E, generator=gen), dim=1)[0]
+    l[50:100] = 36.0 + 24.0 * torch.rand(50, E, generator=gen)
+    l[100:150, :48] = randn(gen, 50, 48)                   # few next to one
+    l[150:] = randn(gen, 50, E, scale=40.0)
+    same(gpu_lib, l.to(dtype), 6, scores="sigmoid", n_groups=n_groups, top_groups=top_groups, group_top=group_top)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("scores", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("n_groups,top_groups,group_top", GROUPS)
+def test_logits_next_to_zero(gpu_lib, dtype, scores, n_groups, top_groups, group_top):
+    """Logits whose scores are one number in float64 (below 2^-55: every exponential is 1 and every sigmoid 1/2), subnormal ones and both zeros among them,
+    and logits around 2^-36, whose scores float64 tells apart where their type does: by 2^-45 at least, 2^-53 being float64's unit there."""
+    gen = torch.Generator().manual_seed(n_groups)
+    T, E = 120, 64
+    tiny = torch.finfo(dtype).smallest_normal
+    kinds = [torch.sign(randn(gen, T // 3, E)) * (2.0 ** -70 if dtype is not F16 else 0.0) * (1.0 + torch.rand(T // 3, E, generator=gen)),
+             randn(gen, T // 3, E, scale=tiny / 4) if dtype is not F16 else torch.sign(randn(gen, T // 3, E)) * 0.0,
+             torch.sign(randn(gen, T // 3, E)) * 2.0 ** (-36 if dtype is not F16 else -20) * (1.0 + torch.round(64 * torch.rand(T // 3, E, generator=gen)) / 64)]
+    if group_top == 2:
+        kinds.pop()                                        # (sums of different scores that differ in the last place, if at all)
+    l = torch.cat(kinds).to(dtype)
+    l[::5] = torch.sort(l[::5].float(), dim=1)[0].to(dtype)  # (the larger ones at the higher ids)
+    same(gpu_lib, l, 6, scores=scores, n_groups=n_groups, top_groups=top_groups, group_top=group_top)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("scores", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("n_groups,top_groups,group_top", GROUPS)
+def test_more_equal_logits_than_choices(gpu_lib, dtype, scores, n_groups, top_groups, group_top):
+    """The last choice is one of many equal logits, and others that are smaller have its score and lower ids: zeros of the other sign, 0 beside 2^-70."""
+    E = 64
+    rows = []
+    for most, few in ((0.0, -0.0), (-0.0, 0.0), (2.0 ** -70, 0.0), (2.0 ** -70, -0.0), (0.0, -2.0 ** -70), (2.0 ** -70, 2.0 ** -71), (2.0 ** -24, 0.0), (1.0, 0.5),
+                      (0.0, -2.0 ** -24), (2.0 ** -27, 2.0 ** -28), (2.0 ** -60, 2.0 ** -130)):
+        for first in (0, 1, 8, 19):
+            l = torch.full((E,), most)
+            l[first:first + 8] = few                       # (a whole group, and parts of two)
+            if first == 1:
+                l[40:] = 3.0
+                l[50] = few
+            rows.append(l)
+    same(gpu_lib, torch.stack(rows).to(dtype), 6, scores=scores, n_groups=n_groups, top_groups=top_groups, group_top=group_top)
