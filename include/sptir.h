@@ -633,7 +633,7 @@ sptir_status_t sptir_moe_product(const sptir_moe_routing_t* routing, const sptir
  * The experts' products of 8-bit integers.  X and W of `product` hold int8 values (any, -128 too); x and W[e] are these times x_scales[row of X]
  * and w_scales[e * w_scales_stride + row of W[e]]: a scale for each token and one for each output channel (swiglu: 2 * d_out).
  * `type` is that of Y, bias, residual and pre.  Sums are whole numbers without rounding, d_in at most 131071 (UNSUPPORTED beyond); z is
- * (the sum * x's scale) * W's scale + bias in float32.  Everything else as sptir_moe_product.
+ * (the sum * x's scale) * W's scale + bias in float32, with d_in 0 the bias.  Everything else as sptir_moe_product.
  */
 sptir_status_t sptir_moe_product_int8(const sptir_moe_routing_t* routing, const sptir_moe_product_t* product, const float* x_scales,
                                       const float* w_scales, int64_t w_scales_stride, void* stream);

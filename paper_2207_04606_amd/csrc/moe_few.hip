@@ -125,7 +125,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_moe_few(MoeProduct p, int32_t a
   float of_row = 0.f, of_column[kGated ? 2 : 1][4] = {};
   if constexpr (kInt8) {
     const int piece = (int)threadIdx.x >> 6, f = kGated ? piece : piece / kFN, g = kGated ? 0 : piece % kFN;
-    if (!none && piece < kPieces) {
+    if (!none && piece < kPieces && p.n_r > 0) {  // (otherwise no scale belongs to a sum, and z is the bias)
       of_row = p.a_scales[x_row(p, min(t.first + 16 * f + fr, t.end - 1))];
       const float* at = p.b_scales + t.expert * p.b_scales_stride;
 #pragma unroll
