@@ -184,7 +184,8 @@ extern "C" int64_t sptir_moe_product_dw_workspace(int64_t n_rows, int32_t n_expe
 }
 
 extern "C" int64_t sptir_moe_product_dw_packed_workspace(int32_t type, int64_t x_rows, int64_t n_rows, int32_t n_experts, int32_t d_in, int32_t d_z) {
-  if (!moe_type_ok(type) || x_rows <= 0 || x_rows >= (int64_t)INT32_MAX || n_rows <= 0 || n_rows >= (int64_t)INT32_MAX || d_in <= 0) return 0;
+  if (!moe_type_ok(type) || x_rows <= 0 || x_rows >= (int64_t)INT32_MAX || n_rows <= 0 || n_rows >= (int64_t)INT32_MAX || d_in < 0) return 0;
+  if (d_in == 0) return sptir_moe_product_dw_workspace(n_rows, n_experts, d_in, d_z);  // (db alone: there is no x)
   if (n_experts <= 0 || n_experts > kMoeMaxExperts || d_in > INT32_MAX / 4 || d_z <= 0 || d_z > INT32_MAX / 4) return 0;  // (nothing to do, or the call is refused)
   return unpacked_at(n_rows, n_experts, d_in, d_z) + x_rows * unpacked_columns(type, d_in) * moe_type_bytes(type);
 }
