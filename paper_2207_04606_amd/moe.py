@@ -320,10 +320,10 @@ def sptir_moe_combine_backward(routing: MoeRouting, dY, Ys, weights, dYs, d_weig
     _check(st, "sptir_moe_combine_backward")
 
 
-def _here(*tensors):
-    """A call runs on the current device, and so are its tensors."""
+def _here(*tensors, routing=None):
+    """A call runs on the current device, and so are its tensors and the arrays of its routing."""
     device = torch.cuda.current_device()
-    for t in tensors:
+    for t in tensors if routing is None else (*tensors, routing.expert_ptr, routing.entry_of):
         if t is not None and t.get_device() != device:
             raise ValueError(f"a tensor is on {t.device}, the current device is {device}")
 
@@ -491,7 +491,7 @@ def sptir_moe_product_int8(routing: MoeRouting | None, X, x_scales, W, w_scales,
     r, ldr = _matrix(residual, dtype, rows, d_out, "residual")
     z, ldz = _matrix(pre, dtype, rows, wide, "pre")
     y, ldy = _matrix(Y, dtype, rows, d_out, "Y")
-    _here(X, x_scales, W, w_scales, Y, bias, residual, pre)
+    _here(X, x_scales, W, w_scales, Y, bias, residual, pre, routing=routing)
     q = _Product(_PRODUCT_SIZE, kind, act, 1 if gather else 0, d_in, d_out, rows, x, ldx, w, ldw, w_stride, b, b_stride, r, ldr,
                  z, ldz, y, ldy)
     st = lib.sptir_moe_product_int8(routing._ref if routing is not None else None, ctypes.byref(q), _vector(x_scales, x_rows, "x_scales"),
@@ -548,7 +548,7 @@ def sptir_moe_product_dx_packed(routing: MoeRouting | None, dZ, W, dX, pre, expo
     z, ldz = _matrix(pre, torch.int8, rows, wide, "pre")
     e, lde = _exponents(exponents, rows, wide, "exponents")
     dx, ld_dx = _matrix(dX, dtype, rows, wide, "dX")
-    _here(dZ, W, dX, pre, exponents)
+    _here(dZ, W, dX, pre, exponents, routing=routing)
     q = _ProductDx(_PRODUCT_DX_SIZE, kind, act, 0, d_in, d_z, rows, dz, ld_dz, w, ldw, w_stride, z, ldz, dx, ld_dx)
     _check(lib.sptir_moe_product_dx_packed(routing._ref if routing is not None else None, ctypes.byref(q), e, lde, _stream_ptr(stream)),
            "sptir_moe_product_dx_packed")
@@ -569,7 +569,7 @@ def sptir_moe_product_dw_packed(routing: MoeRouting | None, dZ, X, exponents, dW
     x, ldx = _matrix(X, torch.int8, x_rows, d_in, "X")
     e, lde = _exponents(exponents, x_rows, d_in, "exponents")
     b, b_stride = _experts_vector(db, dtype, E, d_z, "db")
-    _here(dZ, X, exponents, dW, db)
+    _here(dZ, X, exponents, dW, db, routing=routing)
     ws = _workspace(lib.sptir_moe_product_dw_packed_workspace(kind, x_rows, rows, E, d_in, d_z), stream)
     q = _ProductDw(_PRODUCT_DW_SIZE, kind, 1 if gather else 0, 0, d_in, d_z, rows, dz, ld_dz, x, ldx, w, ldw, w_stride, b, b_stride,
                    ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0)
