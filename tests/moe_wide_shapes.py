@@ -17,3 +17,8 @@ def tiles(rows, cols):
 def columns(d_out, activation):
     """of y, twice as many as a tile takes where gates and what goes with them lie side by side"""
     return 2 * d_out if activation == "swiglu" else d_out
+# through a z kept in 8 bits: several activations of a shape; a second half of swiglu's that begins inside a block of 32 columns
+DX_KEPT = [(3700, 1, 0, 7640, 328, ("relu", "swiglu"), 0.0), (2050, 2, 3, 6640, 584, ("gelu", "silu"), 0.1), (4100, 1, 2, 7112, 776, ("swiglu", "silu"), 0.2)]
+# 8-bit integers, of which a step takes 128 of r: inputs that end inside a step, experts whose last tiles are ragged, rows of no expert between them
+INT8 = [(3700, 1, 0, 656, 7640, "none", 0.0), (4000, 1, 0, 912, 8120, "gelu", 0.0), (4000, 1, 0, 656, 4040, "swiglu", 0.0),
+        (2050, 2, 3, 528, 6640, "relu", 0.1), (4100, 1, 2, 1552, 7112, "silu", 0.2), (2000, 2, 4, 1040, 3400, "swiglu", 0.1)]
