@@ -71,6 +71,22 @@ def test_groups_of_biases_past_the_keys(gpu_lib, scores):
         same(gpu_lib, randn(gen, 50, 8 * each), 2, bias=bias, scores=scores, n_groups=8, top_groups=3, group_top=2)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scores", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("group_top", [1, 2])
+def test_padding_beside_other_tokens(gpu_lib, dtype, scores, group_top):
+    """Tokens without any candidate, in every place of a wavefront, beside some with as many groups as stay and fewer."""
+    gen = torch.Generator().manual_seed(group_top)
+    T, E, G = 300, 64, 8
+    l = randn(gen, T, E, scale=2.0)
+    for t in range(T):
+        for g in range(G):
+            if (t * 7 + g * 3) % 8 < t % 9:
+                l[t, g * 8:g * 8 + 8] = -math.inf
+    for bias in (None, 0.1 * randn(gen, E)):
+        same(gpu_lib, l.to(dtype), 4, bias=bias, scores=scores, n_groups=G, top_groups=3, group_top=group_top)
+
+
 # ------------------------------------------------------------------------------------------------ 16-bit logits as keys
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
 @pytest.mark.parametrize("n_groups,top_groups,group_top", GROUPS)
@@ -121,3 +137,19 @@ def test_more_equal_logits_than_choices(gpu_lib, dtype, scores, n_groups, top_gr
                 l[50] = few
             rows.append(l)
     same(gpu_lib, torch.stack(rows).to(dtype), 6, scores=scores, n_groups=n_groups, top_groups=top_groups, group_top=group_top)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("n_groups,top_groups,group_top", GROUPS)
+def test_softmaxes_that_float64_cannot_hold(gpu_lib, dtype, n_groups, top_groups, group_top):
+    """Exponents of -600 and beyond: of those below -750 nothing is left, and they tie."""
+    gen = torch.Generator().manual_seed(n_groups)
+    T, E = 120, 64
+    l = -500.0 - 400.0 * torch.rand(T, E, generator=gen)
+    l[40:80] = -760.0 - 400.0 * torch.rand(40, E, generator=gen)
+    l[80:] *= 60.0
+    # (none whose exponential has few digits left: one more or less of them is the last place of the library's)
+    l = torch.where((l < -700.0) & (l > -750.0), -650.0, l)
+    l = torch.sort(l, dim=1)[0]
+    l[:, 5] = 0.0
+    same(gpu_lib, l.to(dtype), 6, scores="softmax", n_groups=n_groups, top_groups=top_groups, group_top=group_top)
