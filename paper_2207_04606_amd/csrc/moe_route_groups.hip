@@ -29,9 +29,10 @@ struct Scoring {
 // keys that are further apart than 2^-16 of the larger one, or with a bias than 2^-17 (1 + the larger one), say how c lie.  Tokens with two choices
 // closer than that (of 256 experts one in a hundred) are put in order by float64; those whose groups are, or whose keys float32 has no room for, are chosen from in float64
 // altogether, with the other tokens of the wavefront.
-// Logits of 16 bits without a bias are keys themselves, and ties are ties: a mark takes nothing from them, and both zeros are one.  Float64 tells their scores
-// apart while exponents are within +- 600, sigmoids' logits below 30 and differences not below 2^-40.  Of equal ones, which their type's step (2^-11 of them at
-// least) keeps that far from the next, that holds down to 2^-28; of smaller ones where no logit but zero is as small.
+// Logits of 16 bits without a bias are keys themselves, and ties are ties: a mark takes nothing from them.  Float64 tells their scores
+// apart while exponents are within +- 600, sigmoids' logits below 30 and differences not below 2^-40.  Where the last choice is one of more equal ones than there
+// are choices, that has to hold for the next smaller one too: their type's step (2^-11 of them at least) sees to it down to 2^-28, and for smaller ones the
+// token must have no other logit as small (a zero of the other sign is one).
 constexpr float kFar = 0x1p100f;  // past all keys
 constexpr float kMost = 0x1p90f;  // keys are cut off here, and a choice past 2^80 is left to float64
 constexpr float kSmall = 0x1p-28f;
@@ -166,7 +167,7 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
     const bool logit_keys = sizeof(T) == 2 && !how.bias, sums = how.group_top == 2;
     auto take_logits = [&] {
 #pragma unroll
-      for (int c = 0; c < C; ++c) key[c] = key[c] == -kFar ? -kFar : fminf(fmaxf(l[c] + 0.f, -kMost), kMost);  // (-0 + 0 is 0)
+      for (int c = 0; c < C; ++c) key[c] = key[c] == -kFar ? -kFar : fminf(fmaxf(l[c], -kMost), kMost);
     };
     // whether float64 may not tell the score of such a key from that of one `gap` below
     auto unclear = [&](float logit, float gap) {
@@ -228,7 +229,7 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
 #pragma unroll
     for (int c = 0; c < C; ++c) order[c] = marked_key<C>(key[c], c);
     // One choice more than there are, for the distance of the last; as long as it is too close, one more.  The choices are the lanes'.
-    float last = 0.f;
+    float last = 0.f, top = 0.f;
     bool tight = false, more = true;
     int many = 0;  // choices that are further apart from the rest
     for (int j = 0;; ++j) {
@@ -238,12 +239,11 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
       const int32_t cut = best & ~15, most_cut = lanes_max<L>(cut);
       const int owner = __ffsll(lanes_of<L>(__ballot(cut == most_cut), base)) - 1;
       const int at = 15 - (lanes_max<L>(lane == owner ? best : INT32_MIN) & 15);
-      const float top = of_key(most_cut);
+      top = of_key(most_cut);
       const bool some = top > -0.5f * kFar;
       bool apart = j > 0;
       if (some && logit_keys) {
         unsure = unsure || (more && unclear(top, j > 0 ? last - top : 0.f));
-        small = small || (more && j >= top_k && last == top && fabsf(top) < kSmall);
       } else if (some) {
         const float larger = fmaxf(fabsf(last), fabsf(top));
         unsure = unsure || (more && larger > 0x1p80f);
@@ -265,17 +265,16 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
 #pragma unroll
       for (int c = 0; c < C; ++c) order[c] = order[c] == taken ? INT32_MIN : order[c];
     }
-    // (Float16 has no logit but zero that is as small.)
-    if constexpr (std::is_same_v<T, __bf16>) {
-      if (__ballot(small)) {
-        float again[C];
-        read_logits<T, C>(row, first, n_experts, again);
-        bool other = false;
+    // (Of such keys the rounds end with one more than there are choices, and the last two of a token tell whether they are equal.)
+    if (sizeof(T) == 2 && __ballot(logit_keys && (small || (last == top && fabsf(top) < kSmall)))) {
+      small = small || (last == top && fabsf(top) < kSmall);
+      float again[C];
+      read_logits<T, C>(row, first, n_experts, again);
+      bool other = false;
 #pragma unroll
-        for (int c = 0; c < C; ++c) other = other || (again[c] != 0.f && fabsf(again[c]) < kSmall);
-        const bool others = lanes_of<L>(__ballot(other), base) != 0;
-        unsure = unsure || (small && others);
-      }
+      for (int c = 0; c < C; ++c) other = other || (fabsf(again[c]) < kSmall && __builtin_bit_cast(uint32_t, again[c]) != 0);
+      const bool others = lanes_of<L>(__ballot(other), base) != 0;
+      unsure = unsure || (small && others);
     }
     // Those that are close are put in order by what they are in float64 (without a bias softmaxes by their exponentials).
     unsure = unsure || (tight && !how.sigmoid && how.bias);
