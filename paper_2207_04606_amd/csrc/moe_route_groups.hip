@@ -27,8 +27,9 @@ struct Scoring {
 // A key is c with the last four bits taken for a mark, by which the largest of a lane's keys is the one of the lowest number.  Errors: a sigmoid
 // 2^-21 s, a softmax 2^-21 s and 2^-24 times its exponent (up to 70, for keys of 2^-100 and more) more, the sum 2^-24 |c|, the mark 2^-19 |c|.  So two
 // keys that are further apart than 2^-16 of the larger one, or with a bias than 2^-17 (1 + the larger one), say how c lie.  Tokens with two choices
-// closer than that (of 256 experts one in a hundred) are put in order by float64; those whose groups are, or whose keys float32 has no room for, are chosen from in float64
-// altogether, with the other tokens of the wavefront.
+// closer than that (of 256 experts one in a hundred) are put in order by float64.  Chosen from in float64 altogether, with the other tokens of the wavefront,
+// are those whose groups are close (with a bias 2^-19 (1 + the largest) for sigmoids and 2^-18 for softmaxes, without one 2^-16 of the larger score), whose
+// keys float32 has no room for, softmaxes with a bias that have a close choice, and, where groups are told apart by such keys, tokens without any candidate.
 // Logits of 16 bits without a bias are keys themselves, and ties are ties: a mark takes nothing from them.  Float64 tells their scores
 // apart while exponents are within +- 600, sigmoids' logits below 30 and differences not below 2^-40.  Where the last choice is one of more equal ones than there
 // are choices, that has to hold for the next smaller one too: their type's step (2^-11 of them at least) sees to it down to 2^-28, and for smaller ones the
@@ -102,7 +103,7 @@ __device__ inline void take_two(V v, V& best, V& second) {
 }
 
 // L lanes per token, lane l has the experts l * C .. l * C + C - 1 (as k_moe_route).  Bound by instructions: k + 1 rounds over the C keys of a lane, and
-// by the slowest wavefront, one that chooses in float64 (an eighth of the time).  16,384 tokens of 256 experts: 8 groups 19 us, no groups 15; the logits'
+// by the slowest wavefront, one that chooses in float64 (an eighth of the time).  16,384 tokens of 256 experts: 8 groups 18 to 20 us, no groups 15; the logits'
 // bytes alone 3.5.  (All in float64: 33.)
 template <typename T, int L, int C>
 __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ logits, int64_t ld, int32_t n_tokens, int32_t n_experts,
@@ -373,7 +374,7 @@ __global__ __launch_bounds__(256) void k_moe_route_groups(const T* __restrict__ 
 // With p = w / scale and m = sum w dw over the choices:
 //   softmax, normalised   dl = w (dw - m / scale) of a choice, others 0;   not   w dw - p m, others -p m, p of all experts
 //   sigmoid, normalised   dl = w (dw - m / scale) (1 - s);                 not   w dw (1 - s)
-// Bound by memory: 16,384 tokens of 256 experts of float32 5.9 us, 33.6 MB of logits and gradients (the logits from the memory-side cache).
+// Bound by memory: 16,384 tokens of 256 experts of float32 5.1 to 5.9 us, 33.6 MB of logits and gradients (the logits from the memory-side cache).
 template <typename T, int L, int C>
 __global__ __launch_bounds__(256) void k_moe_route_groups_backward(const T* __restrict__ logits, int64_t ld, int32_t n_tokens,
                                                                    int32_t n_experts, int32_t top_k, Scoring how,

@@ -234,7 +234,7 @@ __device__ inline void moe_clear_8(const MoeProduct& p, int64_t i, int32_t j, in
   if (kOp == kMoeDx && kEnd == kEndSwiglu) write_8<T, kWords>((T*)p.C + i * p.ldc + j + p.n_j, many, zero);
 }
 
-constexpr int kMoeStep = 64;  // most of r that a step takes
+constexpr int kMoeStep = 64;  // most lines across that a step takes (dx, dw; of 8-bit integers, which lie along r, it takes 128 of r)
 // the tiles' kernels count 16-byte words of an operand (of a step's lines, where they lie across) with 32 bits
 inline bool moe_near_elements(int in_word, int64_t rows, int64_t ld) { return rows == 0 || ld < ((int64_t)1 << 32) * in_word / rows; }
 inline bool moe_near(int32_t type, int64_t rows, int64_t ld) { return moe_near_elements(16 / moe_type_bytes(type), rows, ld); }

@@ -9,9 +9,10 @@
 // 237 us, 1160, the gradients 1220 and 1270; of 8-bit integers 440 us, 2500 TOP/s (the library's 2050), and 144 us, 1910.  With short
 // ones (r = 1024) the step's loads are not there in time, since all workgroups ask memory for new operands at once, and the epilogue is a sixth of the tile:
 // 32,768 rows, 1024 x 2048, 140 us, 980.
-// The gradients of 16 bits lose more where experts have different rows (32,768 rows of 32 experts, 2048 x 1024: dX 188 us, dW 187, 730 TFLOP/s; matrix instructions fill
-// 34 % of a CU's clocks in dW): tiles of 600 to 3000 rows do not come out even over four turns (a sixth of dW by the rows' numbers); 4 to 8 % of the clocks are
-// LDS bank conflicts; and the wide kernels spill at the change of tile (dW 10 registers, 22 with db; dX 10 to 16), where every reload waits for all loads too.
+// The gradients of 16 bits lose more where experts have different rows (32,768 rows of 32 experts, 2048 x 1024: dX 188 us, dW 192, 720 TFLOP/s, of rows gathered and
+// with db 216 to 222; where every expert has 1024 rows 159, 171 and 199; matrix instructions fill 34 % of a CU's clocks in dW): tiles of 600 to 3000 rows do not come out even over four turns (a sixth of dW by the rows' numbers); 4 to 8 % of the clocks are
+// LDS bank conflicts; and the wide kernels spill at the change of tile (dW 10 registers, 22 with db; dX 10 to 16, through a z kept in 8 bits 16 to 23;
+// 8-bit integers up to 7, with float32 results 9 to 18), where every reload waits for all loads too.
 // The derivative of an activation is arithmetic that no matrix instructions run beside, unless the CU's other workgroup has some: 11 us of a narrow tile with
 // gelu (8192 x 1024 x 4096: 73 us without, 84 with it), whether z has 16 bits or 8.
 // float32 is bound by its instructions: 4096 x 4096 x 4096 1040 us, 132 TFLOP/s (a library product: 150).  Operands that do not

@@ -555,7 +555,8 @@ def sptir_moe_product_dx_packed(routing: MoeRouting | None, dZ, W, dX, pre, expo
 
 
 def sptir_moe_product_dw_packed(routing: MoeRouting | None, dZ, X, exponents, dW, db=None, gather: bool = False, stream=None) -> None:
-    """sptir_moe_product_dw with the X that sptir_moe_pack kept: int8 codes and their exponents."""
+    """sptir_moe_product_dw with the X that sptir_moe_pack kept: int8 codes and their exponents.  (For the time of the call it takes
+    memory for X in its type.)"""
     lib = _ready or _library()
     kind = _type(dZ, "dZ")
     dtype = dZ.dtype
