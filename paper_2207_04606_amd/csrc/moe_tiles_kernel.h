@@ -262,11 +262,13 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   // gathered for dW of 2048 x 1024 and 32 experts 305 -> 207 us.)
   uint32_t x_row[kOp == kMoeDw ? kLoadsB : 1] = {};
   auto find_rows = [&](int step) __attribute__((always_inline)) {
-    each<kLoadsB>([&](auto n) {
-      x_row[n] = (uint32_t)(p.entry_of ? moe_token(p, entry[n]) : r0 + (int64_t)step * kBR + b_line(n));
-      asm volatile("" : "+v"(x_row[n]));
-    });
-    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (kOp == kMoeDw) {
+      each<kLoadsB>([&](auto n) {
+        x_row[n] = (uint32_t)(p.entry_of ? moe_token(p, entry[n]) : r0 + (int64_t)step * kBR + b_line(n));
+        asm volatile("" : "+v"(x_row[n]));
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
   // (without kWords) the length of the n-th chunk's line, and how far the chunk's end is past its end
   auto line_length = [&](int n) { return n < kLoadsA ? (kAAlongR ? p.n_r : p.n_i) : (kBAlongR ? p.n_r : p.n_j); };
@@ -306,7 +308,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void k_moe_tiles(Moe
   };
   auto load = [&](int step, int into) __attribute__((always_inline)) {
     const bool whole = kWords && (int64_t)(step + 1) * kBR <= r1 - r0;
-    if constexpr (kOp == kMoeDw) find_rows(step);
+    find_rows(step);
     if (whole) each<kLoads>([&](auto n) { load_one(step, into, n, std::true_type{}); });
     else each<kLoads>([&](auto n) { load_one(step, into, n, std::false_type{}); });
     if constexpr (kWords) {
